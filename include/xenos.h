@@ -79,15 +79,20 @@ enum {
     XENOS_OP_MAC = 12,            /* x.mac: three inputs of equal shape, a * b + c element-wise (product rounded, then sum) */
     XENOS_OP_TRANSPOSE = 13,      /* x.transpose of a matrix: (c, h, 1) -> (h, c, 1), y[r][q] = x[q][r] */
     XENOS_OP_SPLIT = 14,          /* x.split, one part per call: channels [pad, pad + cout) of the input */
-    XENOS_OP_MATMUL = 15          /* x.matmul: A (h rows x c columns, or a vector) times the constant matrix
+    XENOS_OP_MATMUL = 15,         /* x.matmul: A (h rows x c columns, or a vector) times the constant matrix
                                      `weight` = B [c][cout] row-major, plus `bias` [cout] if given; the
                                      result has cout columns.  MatmulX -> MatmulY (Table 1): two such products
                                      with no activation between them are linked by multiplying the constants
                                      when that does not add work */
+    /* Row operators (no counterpart in Table 3: what a language model's head needs beside x.matmul).  A row is the c
+     * channels of one pixel of an NHWC tensor, of a matrix or of a vector; see "Row operators" below. */
+    XENOS_OP_LAYERNORM = 16,      /* (x - mean) / sqrt(var + bn_eps) * weight + bias over each row: weight [c], bias [c] or NULL */
+    XENOS_OP_QMATMUL = 17,        /* xenos_graph_add_qmatmul */
+    XENOS_OP_LOGPROB = 18         /* xenos_graph_add_logprob */
 };
 
 enum { XENOS_ACT_NONE = 0, XENOS_ACT_RELU = 1, XENOS_ACT_RELU6 = 2 };
-enum { XENOS_DTYPE_F32 = 0, XENOS_DTYPE_BF16 = 1 };
+enum { XENOS_DTYPE_F32 = 0, XENOS_DTYPE_BF16 = 1, XENOS_DTYPE_I32 = 2 };      /* I32: labels and ids of LOGPROB only */
 enum { XENOS_LAYOUT_NCHW = 0, XENOS_LAYOUT_NHWC = 1 };
 
 /* Arithmetic of a compiled graph.
@@ -133,7 +138,9 @@ XENOS_API xenos_status_t xenos_graph_create(const xenos_hw_info_t *hw, xenos_gra
  * dtype / layout describe the caller's device buffer handed to xenos_graph_run:
  * FP32_CUDA_CORE graphs take F32 NCHW; BF16_TENSOR graphs take F32 or BF16 NCHW when the
  * input feeds a convolution with fewer than 8 input channels (an image), BF16 NHWC with a
- * channel count that is a multiple of 8 otherwise. */
+ * channel count that is a multiple of 8 otherwise.  Inputs that only row operators read may be
+ * F32 or BF16 NHWC with any channel count (NCHW when h = w = 1, which is the same memory).  The labels of a LOGPROB
+ * are I32 NHWC in either precision. */
 XENOS_API xenos_status_t xenos_graph_add_input(xenos_graph_t *g, int32_t dtype, int32_t layout,
                                                int32_t c, int32_t h, int32_t w, xenos_id_t *tensor);
 
@@ -145,9 +152,50 @@ XENOS_API xenos_status_t xenos_graph_add_op(xenos_graph_t *g, const xenos_op_des
 
 /* Mark a tensor as a graph output.  The caller's buffer is dense: feature maps
  * [batch][C][H][W] (NCHW) or [batch][H][W][C] (NHWC), vectors [batch][C].
- * FP32 graphs: F32 NCHW.  BF16 graphs: vectors F32; feature maps BF16 NHWC. */
+ * FP32 graphs: F32 NCHW.  BF16 graphs: vectors F32; feature maps BF16 NHWC; results of LAYERNORM and QMATMUL also F32
+ * NHWC (only row operators of the graph may then read them too).  Results of LOGPROB: F32, ids I32, NHWC. */
 XENOS_API xenos_status_t xenos_graph_mark_output(xenos_graph_t *g, xenos_id_t tensor,
                                                  int32_t dtype, int32_t layout);
+
+/* Row operators
+ *
+ * In BF16_TENSOR graphs rows are bf16 or, as graph inputs and between row operators where noted, fp32; arithmetic is fp32.  In
+ * FP32_CUDA_CORE graphs LAYERNORM and LOGPROB take tensors whose channels are contiguous (vectors, maps of one pixel;
+ * XENOS_E_UNSUPPORTED otherwise) and QMATMUL, a tensor-core product, is refused (XENOS_E_UNSUPPORTED).  All three are per row: a NaN or an
+ * infinity reaches the results of its row and of no other.  They have no explicit split (XENOS_E_BAD_SPLIT).
+ *
+ * LAYERNORM goes through xenos_graph_add_op: weight = gamma [c], bias = beta [c] or NULL, bn_eps > 0.  The variance is the mean of the
+ * squared deviations.  LAYERNORM -> QMATMUL is a link: the normalised row leaves as 8-bit values with its scale.
+ *
+ * QMATMUL: y[n] = act(sx * scale[n] * sum_k q[k] weight[n][k] + bias[n]) with q = round(127 x / a), halves to even, a = max_k |x[k]|,
+ * sx = a / 127 for every row by itself; a row of zeros gives act(bias), a row with a NaN or an infinity gives NaN.  The sum of
+ * products is exact (c <= 131072).  Weights are constants, given either as weight_i8 [cout][c] with scale [cout], or as fp32 weight
+ * [cout][c], which the library rounds the same way (scale NULL).  The result has cout channels; a RELU or RELU6 record behind it is fused.
+ * Errors: XENOS_E_INVALID (NULL or non-finite parameter, both or neither weights), XENOS_E_SHAPE (cout < 1), XENOS_E_UNSUPPORTED
+ * (c > 131072), at compile as above. */
+typedef struct {
+    int32_t cout, act;
+    const float *weight;          /* [cout][c], or NULL */
+    const int8_t *weight_i8;      /* [cout][c], or NULL */
+    const float *scale;           /* [cout] with weight_i8, else NULL */
+    const float *bias;            /* [cout] or NULL */
+} xenos_qmatmul_desc_t;
+XENOS_API xenos_status_t xenos_graph_add_qmatmul(xenos_graph_t *g, const xenos_qmatmul_desc_t *desc, xenos_id_t input,
+                                                 xenos_id_t *out_tensor);
+
+/* LOGPROB: answers from rows of scores.  logits: any row tensor (scores that an fc, a global pool or a QMATMUL hands to LOGPROB operators alone
+ * stay fp32).  labels: an I32 input of one row of L labels per row of scores, or -1 for none.  top: 0..32 alternatives.
+ * out receives four tensor ids (-1 where there is nothing): out[0] log-probabilities of the labels [L] F32, out[1] entropy in
+ * nats [1] F32, out[2] ids of the `top` best scores [top] I32, in descending order, equal scores in ascending order of their ids,
+ * out[3] their log-probabilities [top] F32.  They have the rows of the logits, can only be graph outputs, and what is not marked as one is not
+ * computed.
+ *  - label -1 (padding) gives 0; any other label outside [0, c) gives NaN and sets the device status XENOS_E_BOUNDS.
+ *  - a score of -inf is masked: probability 0, never an alternative; missing alternatives have id -1 and log-probability -inf.
+ *  - a row with nothing but -inf: log-probabilities -inf, entropy 0, ids -1.
+ *  - a row with a NaN or +inf: log-probabilities and entropy NaN; a NaN is no alternative.
+ * Errors: XENOS_E_INVALID (bad id, top out of range, labels that are no I32 input), XENOS_E_SHAPE (rows differ), at compile as above. */
+XENOS_API xenos_status_t xenos_graph_add_logprob(xenos_graph_t *g, xenos_id_t logits, xenos_id_t labels, int32_t top,
+                                                 xenos_id_t out[4]);
 
 /* Operator linking (Section 4.1, Table 1).
  *  n_ops == 0: automatic scan of the whole graph for every linkable pattern.

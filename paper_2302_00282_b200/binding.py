@@ -21,12 +21,14 @@ E_STATE, E_WORKSPACE, E_CUDA, E_TIMEOUT, E_BOUNDS = -6, -7, -8, -9, -10
 OP_CONV, OP_FC, OP_POOL_MAX, OP_POOL_AVG, OP_POOL_GLOBAL_AVG = 1, 2, 3, 4, 5
 OP_ADD, OP_CONCAT, OP_RELU, OP_RELU6, OP_BATCHNORM = 6, 7, 8, 9, 10
 OP_MUL, OP_MAC, OP_TRANSPOSE, OP_SPLIT, OP_MATMUL = 11, 12, 13, 14, 15
+OP_LAYERNORM, OP_QMATMUL, OP_LOGPROB = 16, 17, 18
 ACT_NONE, ACT_RELU, ACT_RELU6 = 0, 1, 2
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_I32 = 0, 1, 2
 LAYOUT_NCHW, LAYOUT_NHWC = 0, 1
 PRECISION_FP32_CUDA_CORE, PRECISION_BF16_TENSOR = 0, 1
 
 _f32p = ctypes.POINTER(ctypes.c_float)
+_i8p = ctypes.POINTER(ctypes.c_int8)
 
 
 class HwInfo(ctypes.Structure):
@@ -41,7 +43,12 @@ class OpDesc(ctypes.Structure):
                 ("bn_var", _f32p), ("bn_eps", ctypes.c_float)]
 
 
-EXPORTS = ["xenos_graph_create", "xenos_graph_add_input", "xenos_graph_add_op", "xenos_graph_mark_output",
+class QmatmulDesc(ctypes.Structure):
+    _fields_ = [("cout", ctypes.c_int32), ("act", ctypes.c_int32), ("weight", _f32p), ("weight_i8", _i8p), ("scale", _f32p),
+                ("bias", _f32p)]
+
+
+EXPORTS = ["xenos_graph_create", "xenos_graph_add_input", "xenos_graph_add_op", "xenos_graph_add_qmatmul", "xenos_graph_add_logprob", "xenos_graph_mark_output",
            "xenos_graph_link", "xenos_graph_split", "xenos_graph_search_split", "xenos_graph_compile", "xenos_graph_bind", "xenos_graph_run",
            "xenos_graph_profile", "xenos_graph_run_builtin_scratch", "xenos_graph_status", "xenos_graph_selftest_wait_expiry", "xenos_graph_get_plan", "xenos_graph_launch_count", "xenos_graph_save", "xenos_graph_load", "xenos_graph_destroy",
            "xenos_last_error"]
@@ -59,6 +66,8 @@ def lib() -> ctypes.CDLL:
         L.xenos_graph_create.argtypes = [ctypes.POINTER(HwInfo), ctypes.POINTER(vp)]
         L.xenos_graph_add_input.argtypes = [vp, i32, i32, i32, i32, i32, ctypes.POINTER(i32)]
         L.xenos_graph_add_op.argtypes = [vp, ctypes.POINTER(OpDesc), ctypes.POINTER(i32), i32, ctypes.POINTER(i32)]
+        L.xenos_graph_add_qmatmul.argtypes = [vp, ctypes.POINTER(QmatmulDesc), i32, ctypes.POINTER(i32)]
+        L.xenos_graph_add_logprob.argtypes = [vp, i32, i32, i32, ctypes.POINTER(i32)]
         L.xenos_graph_mark_output.argtypes = [vp, i32, i32, i32]
         L.xenos_graph_link.argtypes = [vp, ctypes.POINTER(i32), i32]
         L.xenos_graph_split.argtypes = [vp, i32, i32, i32, i32, i32]
@@ -132,6 +141,36 @@ class Graph:
         t = ctypes.c_int32()
         self._check(lib().xenos_graph_add_op(self._h, ctypes.byref(d), ins, len(inputs), ctypes.byref(t)))
         return t.value
+
+    def add_qmatmul(self, input: int, weight, scale=None, bias=None, act=ACT_NONE) -> int:
+        """weight [cout][c]: int8 with scale [cout], or floats, which the library rounds to 8 bits per output channel."""
+        weight = np.asarray(weight)
+        if weight.ndim != 2:
+            raise ValueError("weight must be a matrix [cout][c]")
+        d = QmatmulDesc()
+        d.cout, d.act = weight.shape[0], act
+        if weight.dtype == np.int8:
+            w = np.ascontiguousarray(weight)
+            d.weight_i8 = w.ctypes.data_as(_i8p)
+        else:
+            w = np.ascontiguousarray(weight, dtype=np.float32)
+            d.weight = _fp(w)
+        s = None if scale is None else np.ascontiguousarray(scale, dtype=np.float32)
+        b = None if bias is None else np.ascontiguousarray(bias, dtype=np.float32)
+        for a, what in ((s, "scale"), (b, "bias")):
+            if a is not None and a.shape != (weight.shape[0],):
+                raise ValueError(f"{what} must have one value per output channel")
+        d.scale, d.bias = _fp(s), _fp(b)
+        t = ctypes.c_int32()
+        self._check(lib().xenos_graph_add_qmatmul(self._h, ctypes.byref(d), input, ctypes.byref(t)))
+        return t.value
+
+    def add_logprob(self, logits: int, labels: Optional[int] = None, top: int = 0):
+        """Returns the tensor ids (log-probabilities of the labels, entropy, ids of the best, their log-probabilities); None
+        in the place of what was not asked for."""
+        out = (ctypes.c_int32 * 4)()
+        self._check(lib().xenos_graph_add_logprob(self._h, logits, -1 if labels is None else labels, top, out))
+        return tuple(None if t < 0 else t for t in out)
 
     def mark_output(self, tensor: int, dtype: int, layout: int):
         self._check(lib().xenos_graph_mark_output(self._h, tensor, dtype, layout))

@@ -91,7 +91,7 @@ xenos_status_t xenos_graph_add_input(xenos_graph_t *gp, int32_t dtype, int32_t l
     Graph &g = gp->g;
     if (g.state != ST_BUILD) return fail(g, XENOS_E_STATE, "add_input after compile");
     if (!tensor) return fail(g, XENOS_E_INVALID, "add_input: tensor is NULL");
-    if ((dtype != XENOS_DTYPE_F32 && dtype != XENOS_DTYPE_BF16) ||
+    if ((dtype != XENOS_DTYPE_F32 && dtype != XENOS_DTYPE_BF16 && dtype != XENOS_DTYPE_I32) ||
         (layout != XENOS_LAYOUT_NCHW && layout != XENOS_LAYOUT_NHWC))
         return fail(g, XENOS_E_INVALID, "add_input: unknown dtype or layout");
     if (c < 1 || h < 1 || w < 1) return fail(g, XENOS_E_SHAPE, "add_input: extents must be positive");
@@ -118,16 +118,36 @@ xenos_status_t xenos_graph_add_op(xenos_graph_t *gp, const xenos_op_desc_t *desc
     XENOS_GUARD_END(gp)
 }
 
+xenos_status_t xenos_graph_add_qmatmul(xenos_graph_t *gp, const xenos_qmatmul_desc_t *desc, xenos_id_t input, xenos_id_t *out_tensor) {
+    if (!gp) return XENOS_E_INVALID;
+    XENOS_GUARD_BEGIN
+    Graph &g = gp->g;
+    if (g.state != ST_BUILD) return fail(g, XENOS_E_STATE, "add_qmatmul after compile");
+    if (!desc || !out_tensor) return fail(g, XENOS_E_INVALID, "add_qmatmul: NULL argument");
+    return append_qmatmul(g, *desc, input, out_tensor);
+    XENOS_GUARD_END(gp)
+}
+
+xenos_status_t xenos_graph_add_logprob(xenos_graph_t *gp, xenos_id_t logits, xenos_id_t labels, int32_t top, xenos_id_t out[4]) {
+    if (!gp) return XENOS_E_INVALID;
+    XENOS_GUARD_BEGIN
+    Graph &g = gp->g;
+    if (g.state != ST_BUILD) return fail(g, XENOS_E_STATE, "add_logprob after compile");
+    if (!out) return fail(g, XENOS_E_INVALID, "add_logprob: NULL argument");
+    return append_logprob(g, logits, labels, top, out);
+    XENOS_GUARD_END(gp)
+}
+
 xenos_status_t xenos_graph_mark_output(xenos_graph_t *gp, xenos_id_t tensor, int32_t dtype, int32_t layout) {
     if (!gp) return XENOS_E_INVALID;
     XENOS_GUARD_BEGIN
     Graph &g = gp->g;
     if (g.state != ST_BUILD) return fail(g, XENOS_E_STATE, "mark_output after compile");
     if (tensor < 0 || tensor >= (int)g.tensors.size()) return fail(g, XENOS_E_INVALID, "mark_output: bad tensor id");
-    if ((dtype != XENOS_DTYPE_F32 && dtype != XENOS_DTYPE_BF16) ||
-        (layout != XENOS_LAYOUT_NCHW && layout != XENOS_LAYOUT_NHWC))
-        return fail(g, XENOS_E_INVALID, "mark_output: unknown dtype or layout");
     Tensor &t = g.tensors[tensor];
+    if ((t.fixed >= 0 ? dtype != t.fixed : dtype != XENOS_DTYPE_F32 && dtype != XENOS_DTYPE_BF16) ||
+        (layout != XENOS_LAYOUT_NCHW && layout != XENOS_LAYOUT_NHWC))
+        return fail(g, XENOS_E_INVALID, "mark_output: unknown dtype or layout, or not the type of the tensor");
     if (t.input_slot >= 0) return fail(g, XENOS_E_INVALID, "mark_output: a graph input cannot be an output");
     if (t.output_slot >= 0) return fail(g, XENOS_E_INVALID, "mark_output: tensor is already an output");
     t.output_slot = (int)g.outputs.size();

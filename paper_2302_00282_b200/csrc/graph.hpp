@@ -24,6 +24,8 @@ struct Tensor {
     int input_slot = -1;          // >= 0: graph input number
     int output_slot = -1;         // >= 0: graph output number
     int io_dtype = XENOS_DTYPE_F32, io_layout = XENOS_LAYOUT_NCHW;   // for graph inputs / outputs
+    int fixed = -1;               // >= 0: result of a LOGPROB, its type whatever the precision
+    int rows() const { return is_vec ? 1 : h * w; }
 };
 
 struct Op {
@@ -34,10 +36,14 @@ struct Op {
     std::vector<float> w, bias, gamma, beta, mean, var;
     float eps = 1e-5f;
     bool has_bias = false, has_bn = false;
+    std::vector<int8_t> q;        // QMATMUL: weights [cout][c]; their scales are in gamma
+    int top = 0;                  // LOGPROB: alternatives
+    int outs[4] = {-1, -1, -1, -1};      // LOGPROB: results (out is the entropy's)
 };
 
 // ---- fused operators (after the CBR pre-fusion) ----------------------------------------------
-enum NodeKind { NK_CONV = 1, NK_DW, NK_FC, NK_MAXPOOL, NK_AVGPOOL, NK_GAP, NK_ADD, NK_CONCAT, NK_MUL, NK_MAC, NK_TRANSPOSE, NK_SLICE };
+enum NodeKind { NK_CONV = 1, NK_DW, NK_FC, NK_MAXPOOL, NK_AVGPOOL, NK_GAP, NK_ADD, NK_CONCAT, NK_MUL, NK_MAC, NK_TRANSPOSE, NK_SLICE,
+                NK_NORM, NK_QMATMUL, NK_LOGPROB };
 
 struct Node {
     int kind = 0;
@@ -48,6 +54,9 @@ struct Node {
     std::vector<float> b;         // folded bias [cout] (zeros when the op had none)
     std::vector<int> user_ops;    // indices of the user ops folded into this node
     int chain = -1;
+    std::vector<int8_t> q;        // qmatmul: weights [cout][cin], scales in w; layer norm: w = gamma, b = beta
+    float eps = 0;
+    int top = 0, outs[4] = {-1, -1, -1, -1};      // logprob
     bool from_matmul = false;     // an x.matmul with a constant right operand (lowered like a pointwise conv / fc)
 };
 
@@ -59,8 +68,9 @@ enum ChainKind {
     CK_CONV_TAIL,           // conv [+ linked shortcut conv] [-> add -> relu] [-> max pool | global avgpool]
     CK_EXPAND_CONCAT,       // {conv1x1, conv3x3} on one input -> concat [-> max pool]
     CK_MATMUL_MATMUL,       // MatmulX -> MatmulY with constant right operands: one product with the constants multiplied
-    CK_CONV_CONV            // ConvX -> ConvY with the intermediate tile in shared memory: conv -> conv1x1 | conv3x3
+    CK_CONV_CONV,           // ConvX -> ConvY with the intermediate tile in shared memory: conv -> conv1x1 | conv3x3
                             // [-> add (identity shortcut)], or squeeze -> {expand1x1 ; expand3x3} -> concat
+    CK_NORM_QMATMUL         // layer norm -> 8-bit product: the row leaves as 8-bit values with its scale
 };
 
 struct SplitRequest { int outc = 0, h = 0, w = 0, k = 1; bool user = false; };
@@ -100,7 +110,11 @@ enum LaunchKind {
     LK_F32_CONV_CONV_POOL, // fp32 linked chain
     LK_F32_MULMAC, LK_F32_TRANSPOSE, LK_F32_SLICE,
     LK_GEMM2,             // two linked convolutions, intermediate tile in shared memory (chain2_kernel)
-    LK_STEM3X3            // 3x3 convolution of an NCHW image with at most 4 channels on the CUDA cores (stem3x3_kernel)
+    LK_STEM3X3,           // 3x3 convolution of an NCHW image with at most 4 channels on the CUDA cores (stem3x3_kernel)
+    LK_ROWS,              // layer norm of rows and / or their rounding to 8 bits (row_kernel)
+    LK_Q8,                // 8-bit product on the tensor cores (q8_tc_kernel)
+    LK_Q8_SMALL,          // 8-bit product of at most 16 rows (q8_small_kernel)
+    LK_LOGPROB            // answers from rows of scores (logprob_kernel)
 };
 
 struct Launch {
@@ -159,6 +173,12 @@ struct Launch {
     // split scratch, two counters (chunks arrived, chunks reduced) per (row tile, channel tile)
     int ksplit = 1, kb_per = 0;
     size_t split_cnt_off = 0;
+    // ---- row operators
+    int row_norm = 0, row_out = 0, row_in_f32 = 0;     // LK_ROWS: normalise; how a row leaves (xk::RO_*); fp32 rows come in
+    int q_pitch = 0, q8_pair = 0;                      // 8-bit product: bytes of a row of either operand; two CTAs share a tile
+    size_t q_scale_off = 0, scratch_bytes = 0;         // rows' scales behind the 8-bit rows; bytes of the split scratch
+    float eps = 0;
+    int labels = -1, n_labels = 0, top = 0, lp_parts_max = 1, outx[4] = {-1, -1, -1, -1};      // LK_LOGPROB
     // ---- fp32 linked chain (conv kxk -> conv1x1 -> pool)
     int Cmid = 0, K2 = 0, act2 = 0;
     int f32_big = 0, f32_ws = 0, f32_iwp = 0, f32_hp = 0;       // register tile 8 x 4 or 2 x 1, weights in shared memory, row pitches
@@ -223,7 +243,11 @@ struct Graph {
 
 // graph.cpp
 xenos_status_t infer_and_append(Graph &g, const xenos_op_desc_t &d, const int *in, int n_in, int *out);
+xenos_status_t append_qmatmul(Graph &g, const xenos_qmatmul_desc_t &d, int in, int *out);
+xenos_status_t append_logprob(Graph &g, int logits, int labels, int top, int *out);
 xenos_status_t compile_graph(Graph &g, int max_batch, int precision);
+// Type of a tensor's elements in memory, once the operators are fused.
+int elem_dtype(const Graph &g, int t);
 // passes.cpp
 xenos_status_t prefuse(Graph &g);
 xenos_status_t link_pass(Graph &g);
@@ -255,5 +279,37 @@ inline int out_dim(int in, int k, int stride, int pad) {
     return num < 0 ? 0 : num / stride + 1;
 }
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+constexpr int kQ8SmallRows = 16;         // rows up to which q8_small_kernel takes an 8-bit product
+constexpr int kLpCtaEntries = 8192;      // entries above which a row of scores has CTAs of 512 threads, and may have several
+
+// Channel tile of an 8-bit product in tiles of one CTA: modelled cycles.  A block of 128 deep takes the slower of the tensor pipe (2 cycles a
+// column) and the operands' way from L2 (75 bytes a cycle); a tile's fill and epilogue come on top.
+inline double q8_cycles(long long rows, int N, int kblocks, int units, int tile_n) {
+    const double tiles = (double)((rows + 127) / 128) * ((N + tile_n - 1) / tile_n);
+    const double block = tile_n * 2.0 > (16384 + tile_n * 128) / 75.0 ? tile_n * 2.0 : (16384 + tile_n * 128) / 75.0;
+    return (double)(long long)((tiles + units - 1) / units) * (kblocks * block + 300.0 + 6.0 * tile_n) + 1000.0;
+}
+// Shared memory of a launch of q8_tc_kernel: 1024 to align, ring, a 4 KB box and 256 bytes of parameters per epilogue warp, barriers.
+constexpr int kQ8FixedSmem = 1024 + 8 * (4096 + 256) + 256;
+inline int q8_stage_bytes(int tile_n, bool pair) { return 16384 + (pair ? 128 : tile_n) * 128; }
+inline int q8_stages(const xenos_hw_info_t &hw, int tile_n, bool pair) {
+    const int cap = hw.smem_bytes_per_cta < 227 * 1024 ? hw.smem_bytes_per_cta : 227 * 1024, n = (cap - kQ8FixedSmem) / q8_stage_bytes(tile_n, pair);
+    return n > 8 ? 8 : n;
+}
+inline int q8_smem_bytes(const xenos_hw_info_t &hw, int tile_n, bool pair) { return kQ8FixedSmem + q8_stages(hw, tile_n, pair) * q8_stage_bytes(tile_n, pair); }
+inline bool q8_fits(const xenos_hw_info_t &hw, int tile_n, bool pair) { return q8_stages(hw, tile_n, pair) >= 2 && 2 * tile_n <= hw.tmem_columns; }
+inline int q8_tile_n(const xenos_hw_info_t &hw, long long rows, int N, int kblocks, int units) {
+    int best = 32;
+    for (int tn = 64; tn <= 256 && q8_fits(hw, tn, false); tn *= 2)
+        if (q8_cycles(rows, N, kblocks, units, tn) <= q8_cycles(rows, N, kblocks, units, best)) best = tn;
+    return best;
+}
+// ... and of pairs of CTAs with tiles of 256 x 256.
+inline double q8_pair_cycles(long long rows, int N, int kblocks, int units) {
+    const double tiles = (double)((rows + 255) / 256) * ((N + 255) / 256);
+    const int pairs = units / 2 < 1 ? 1 : units / 2;
+    return (double)(long long)((tiles + pairs - 1) / pairs) * (kblocks * 540.0 + 1800.0) + 1500.0;
+}
 
 }  // namespace xenos

@@ -81,15 +81,43 @@ xenos_status_t prefuse(Graph &g) {
         case XENOS_OP_RELU6: {
             if (src < 0 || !sole_consumer_ok(op.in[0]) || g.nodes[src].act != XENOS_ACT_NONE ||
                 !(g.nodes[src].kind == NK_CONV || g.nodes[src].kind == NK_DW || g.nodes[src].kind == NK_FC ||
-                  g.nodes[src].kind == NK_ADD))
+                  g.nodes[src].kind == NK_ADD || g.nodes[src].kind == NK_QMATMUL))
                 return fail(g, XENOS_E_UNSUPPORTED,
-                            "activation that does not directly follow a convolution, fc or add (single consumer) has no kernel");
+                            "activation that does not directly follow a convolution, fc, 8-bit product or add (single consumer) has no kernel");
             Node &n = g.nodes[src];
             n.act = op.kind == XENOS_OP_RELU ? XENOS_ACT_RELU : XENOS_ACT_RELU6;
             g.node_of_tensor[n.out] = -1;
             n.out = op.out;
             n.user_ops.push_back(oi);
             g.node_of_tensor[op.out] = src;
+            break;
+        }
+        case XENOS_OP_LAYERNORM:
+        case XENOS_OP_QMATMUL: {
+            Node n;
+            n.kind = op.kind == XENOS_OP_LAYERNORM ? NK_NORM : NK_QMATMUL;
+            n.in = op.in; n.out = op.out;
+            n.cin = x.c; n.cout = g.tensors[op.out].c; n.act = op.act; n.eps = op.eps;
+            n.w = op.kind == XENOS_OP_LAYERNORM ? op.w : op.gamma;
+            n.q = op.q;
+            n.b.assign(n.cout, 0.0f);
+            if (op.has_bias) n.b = op.bias;
+            n.user_ops.push_back(oi);
+            g.nodes.push_back(std::move(n));
+            g.node_of_tensor[op.out] = (int)g.nodes.size() - 1;
+            break;
+        }
+        case XENOS_OP_LOGPROB: {
+            Node n;
+            n.kind = NK_LOGPROB;
+            n.in = op.in; n.out = op.out;
+            n.cin = x.c; n.cout = g.tensors[op.out].c; n.top = op.top;
+            n.user_ops.push_back(oi);
+            for (int i = 0; i < 4; ++i) {
+                n.outs[i] = op.outs[i];
+                if (op.outs[i] >= 0) g.node_of_tensor[op.outs[i]] = (int)g.nodes.size();
+            }
+            g.nodes.push_back(std::move(n));
             break;
         }
         default: {
@@ -212,6 +240,17 @@ static bool try_match(const LinkCtx &cx, int a, Allowed allowed, Chain &out, boo
         return true;
     }
     // ---- bf16 tensor-core chains -----------------------------------------------------------
+    if (A.kind == NK_NORM) {
+        // the normalised row leaves as the 8-bit values and the scale that the product reads.  A product of few rows rounds its rows by
+        // itself (q8_small_kernel): there the link would only replace its one launch.  (A layer norm whose result others read too is not linked.)
+        const int b = cx.sole(a);
+        if (b < 0 || !allowed(b) || g.nodes[b].kind != NK_QMATMUL) return false;
+        if (by_model && (long long)g.max_batch * g.tensors[A.out].rows() <= kQ8SmallRows) return false;
+        out.kind = CK_NORM_QMATMUL;
+        out.nodes = {a, b};
+        out.pattern = "LayerNorm -> 8-bit product (row-wise producer and consumer)";
+        return true;
+    }
     if (A.from_matmul) {
         // MatmulX -> MatmulY (last row of Table 1) with constant right operands and nothing but a bias between
         // them: (X B1 + b1) B2 + b2 = X (B1 B2) + (b1 B2 + b2).  The constants are multiplied once at compile time
@@ -498,6 +537,7 @@ struct Lower {
         if (g.precision == XENOS_PRECISION_BF16_TENSOR) {
             if (x.input_slot >= 0 && x.io_dtype == XENOS_DTYPE_F32) es = 4;
             if (x.output_slot >= 0 && x.is_vec) es = 4;
+            if (elem_dtype(g, t) != XENOS_DTYPE_BF16) es = 4;
         }
         return (double)g.max_batch * tensor_elems(x) * es;
     }
@@ -506,10 +546,12 @@ struct Lower {
         if (n.kind == NK_CONV) return (double)g.max_batch * o.h * o.w * n.cout * n.cin * n.k * n.k;
         if (n.kind == NK_DW) return (double)g.max_batch * o.h * o.w * n.cout * n.k * n.k;
         if (n.kind == NK_FC) return (double)g.max_batch * n.cout * n.cin;
+        if (n.kind == NK_QMATMUL) return (double)g.max_batch * o.rows() * n.cout * n.cin;
         return 0;
     }
     double node_param_bytes(const Node &n) const {
         if (n.w.empty()) return 0;
+        if (n.kind == NK_NORM || n.kind == NK_QMATMUL) return (double)n.q.size() + 4.0 * (n.w.size() + n.b.size());
         return (double)n.w.size() * esize() + 4.0 * n.b.size();
     }
 
@@ -550,7 +592,7 @@ struct Lower {
             break;
         case NK_GAP:
             L.kind = f32 ? LK_F32_GAP : LK_GAP;
-            L.out_dtype = (f32 || g.tensors[n.out].output_slot >= 0) ? XENOS_DTYPE_F32 : XENOS_DTYPE_BF16;
+            L.out_dtype = (f32 || g.tensors[n.out].output_slot >= 0) ? XENOS_DTYPE_F32 : elem_dtype(g, n.out);
             break;
         case NK_ADD:
             L.kind = f32 ? LK_F32_ADD : LK_ADD;
@@ -592,6 +634,9 @@ struct Lower {
 
     xenos_status_t lower_f32_single(int ci, int ni) {
         const Node &n = g.nodes[ni];
+        if (n.kind == NK_NORM) return lower_norm(ci, ni);
+        if (n.kind == NK_QMATMUL) return lower_qmatmul(ci, -1, ni);
+        if (n.kind == NK_LOGPROB) return lower_logprob(ci, ni);
         if (n.kind == NK_CONV || n.kind == NK_DW || n.kind == NK_FC) {
             Launch L;
             L.nodes = {ni};
@@ -1229,7 +1274,7 @@ struct Lower {
         L.out = last->out;
         const Tensor &ot = g.tensors[L.out];
         L.out_ctot = ot.c; L.out_coff = 0;
-        L.out_dtype = (ot.is_vec && ot.output_slot >= 0) ? XENOS_DTYPE_F32 : XENOS_DTYPE_BF16;
+        L.out_dtype = (ot.is_vec && ot.output_slot >= 0) ? XENOS_DTYPE_F32 : ot.is_vec ? elem_dtype(g, L.out) : XENOS_DTYPE_BF16;
         if (!ot.is_vec && ot.c % 8) return fail(g, XENOS_E_UNSUPPORTED, "bf16 NHWC tensors need a channel count that is a multiple of 8");
         // --- split (Section 4.2.1: output channels first, then rows / columns of the feature map)
         const SplitRequest &rq = ch.split;
@@ -1527,8 +1572,128 @@ struct Lower {
         return XENOS_OK;
     }
 
+    // ---- row operators -----------------------------------------------------------------------
+    // Rows have to lie one behind the other with contiguous channels.
+    xenos_status_t check_rows(int t, const char *who) {
+        const Tensor &x = g.tensors[t];
+        const bool nchw = g.precision == XENOS_PRECISION_FP32_CUDA_CORE || (x.input_slot >= 0 && x.io_layout == XENOS_LAYOUT_NCHW);
+        if (nchw && x.rows() > 1) return fail(g, XENOS_E_UNSUPPORTED, std::string(who) + ": rows of an NCHW tensor of more than one pixel are not contiguous");
+        if ((long long)g.max_batch * x.rows() > (1ll << 30)) return fail(g, XENOS_E_UNSUPPORTED, std::string(who) + ": more than 2^30 rows");
+        return XENOS_OK;
+    }
+    xenos_status_t no_split(int ci) {
+        const SplitRequest &s = g.chains[ci].split;
+        if (s.user && (s.outc > 1 || s.h > 1 || s.w > 1 || s.k > 1)) return fail(g, XENOS_E_BAD_SPLIT, "split: row operators are split by rows and, where those are few, by the kernel itself; no explicit split");
+        return XENOS_OK;
+    }
+    // Layer norm and / or rounding to 8 bits of the rows of tensor t.  out: RO_BF16 (0), RO_F32 (1), RO_Q8 (2).
+    Launch rows_launch(int t, const Node *norm, int out) {
+        const Tensor &x = g.tensors[t];
+        Launch L;
+        L.kind = LK_ROWS;
+        L.in0 = t; L.C = L.K = x.c; L.H = x.h; L.W = x.w;
+        L.rows_per_image = x.rows();
+        L.row_norm = norm != nullptr; L.row_out = out;
+        L.row_in_f32 = elem_dtype(g, t) == XENOS_DTYPE_F32;
+        if (norm) { L.w_off = put_f32(norm->w); L.b_off = put_f32(norm->b); L.eps = norm->eps; }
+        if (out == 2) {
+            L.q_pitch = round_up(x.c, 128);
+            const long long rows = (long long)g.max_batch * L.rows_per_image;
+            L.q_scale_off = align_up((size_t)rows * L.q_pitch, 256);
+            L.scratch_bytes = L.q_scale_off + align_up((size_t)rows * 4, 256);
+        }
+        L.bytes = tbytes(t) + (norm ? 8.0 * x.c : 0.0) + (out == 2 ? (double)g.max_batch * L.rows_per_image * (L.q_pitch + 4) : 0.0);
+        return L;
+    }
+    xenos_status_t lower_norm(int ci, int ni) {
+        const Node &n = g.nodes[ni];
+        if (xenos_status_t st = check_rows(n.in[0], "layernorm")) return st;
+        if (xenos_status_t st = no_split(ci)) return st;
+        Launch L = rows_launch(n.in[0], &n, elem_dtype(g, n.out) == XENOS_DTYPE_F32 ? 1 : 0);
+        L.nodes = {ni};
+        L.out = n.out;
+        L.bytes += tbytes(n.out);
+        push(L, ci);
+        return XENOS_OK;
+    }
+    xenos_status_t lower_qmatmul(int ci, int norm_i, int ni) {
+        const Node &n = g.nodes[ni];
+        const Node *norm = norm_i >= 0 ? &g.nodes[norm_i] : nullptr;
+        const int src = norm ? norm->in[0] : n.in[0];
+        if (g.precision == XENOS_PRECISION_FP32_CUDA_CORE) return fail(g, XENOS_E_UNSUPPORTED, "qmatmul: the 8-bit product belongs to BF16_TENSOR graphs");
+        if (xenos_status_t st = check_rows(src, "qmatmul")) return st;
+        if (xenos_status_t st = no_split(ci)) return st;
+        const long long rows = (long long)g.max_batch * g.tensors[src].rows();
+        Launch L;
+        L.nodes = {ni};
+        L.q_pitch = round_up(n.cin, 128);
+        L.C = n.cin; L.K = n.cout; L.H = g.tensors[src].h; L.W = g.tensors[src].w;
+        L.rows_per_image = g.tensors[src].rows();
+        L.act = n.act;
+        L.out = n.out;
+        L.out_dtype = elem_dtype(g, n.out);
+        L.kblocks = L.q_pitch / 128;
+        // weights [cout][pitch], zeros behind a row: the depth is whole blocks
+        L.w_off = blob_reserve(g, (size_t)n.cout * L.q_pitch);
+        for (int o = 0; o < n.cout; ++o) std::memcpy(g.param_blob.data() + L.w_off + (size_t)o * L.q_pitch, n.q.data() + (size_t)o * n.cin, n.cin);
+        L.w2_off = put_f32(n.w); L.b_off = put_f32(n.b);
+        L.flops = 2.0 * node_macs(n);
+        L.bytes = tbytes(n.out) + node_param_bytes(n);
+        if (!norm && rows <= kQ8SmallRows) {
+            L.kind = LK_Q8_SMALL;
+            L.in0 = src;
+            L.row_in_f32 = elem_dtype(g, src) == XENOS_DTYPE_F32;
+            L.bytes += tbytes(src);
+            push(L, ci);
+            return XENOS_OK;
+        }
+        Launch R = rows_launch(src, norm, 2);
+        R.nodes = {norm ? norm_i : ni};
+        push(R, ci);
+        L.kind = LK_Q8;
+        L.q_scale_off = R.q_scale_off; L.scratch_bytes = R.scratch_bytes;
+        L.bytes += (double)rows * (L.q_pitch + 4);
+        const int units = g.hw.sm_count;
+        if (!q8_fits(g.hw, 32, false)) return fail(g, XENOS_E_UNSUPPORTED, "qmatmul: the described shared memory or tensor memory holds no tile");
+        L.tile_n = q8_tile_n(g.hw, rows, n.cout, L.kblocks, units);
+        L.q8_pair = units >= 2 && q8_fits(g.hw, 256, true) &&
+                    q8_pair_cycles(rows, n.cout, L.kblocks, units) < q8_cycles(rows, n.cout, L.kblocks, units, L.tile_n);
+        if (L.q8_pair) L.tile_n = 256;
+        L.smem_bytes = q8_smem_bytes(g.hw, L.tile_n, L.q8_pair);
+        push(L, ci);
+        return XENOS_OK;
+    }
+    xenos_status_t lower_logprob(int ci, int ni) {
+        const Node &n = g.nodes[ni];
+        if (xenos_status_t st = check_rows(n.in[0], "logprob")) return st;
+        if (xenos_status_t st = no_split(ci)) return st;
+        const Tensor &x = g.tensors[n.in[0]];
+        Launch L;
+        L.kind = LK_LOGPROB;
+        L.nodes = {ni};
+        L.in0 = n.in[0]; L.C = L.K = x.c; L.H = x.h; L.W = x.w;
+        L.rows_per_image = x.rows();
+        L.row_in_f32 = elem_dtype(g, n.in[0]) == XENOS_DTYPE_F32;
+        L.top = n.top;
+        if (n.in.size() > 1) { L.in1 = L.labels = n.in[1]; L.n_labels = g.tensors[n.in[1]].c; }
+        L.bytes = tbytes(n.in[0]) + (L.labels >= 0 ? 4.0 * g.max_batch * L.rows_per_image * L.n_labels : 0.0);
+        for (int i = 0; i < 4; ++i)
+            if (n.outs[i] >= 0 && g.tensors[n.outs[i]].output_slot >= 0) { L.outx[i] = n.outs[i]; L.bytes += tbytes(n.outs[i]); }
+        if (L.outx[2] < 0 && L.outx[3] < 0) L.top = 0;      // (nobody wants the alternatives)
+        L.flops = 5.0 * g.max_batch * L.rows_per_image * x.c;
+        if (x.c > kLpCtaEntries) {
+            L.lp_parts_max = 16;
+            L.scratch_bytes = (size_t)2 * g.hw.sm_count * (16 + 8 * (size_t)L.top);
+        }
+        push(L, ci);
+        return XENOS_OK;
+    }
+
     xenos_status_t lower_bf16_single(int ci, int ni) {
         const Node &n = g.nodes[ni];
+        if (n.kind == NK_NORM) return lower_norm(ci, ni);
+        if (n.kind == NK_QMATMUL) return lower_qmatmul(ci, -1, ni);
+        if (n.kind == NK_LOGPROB) return lower_logprob(ci, ni);
         if (n.kind == NK_CONV) {
             // the first layer at small batch: a 3x3 convolution of an NCHW image runs on the CUDA cores (K = 27 fills
             // less than half of one 64-wide K block of the MMA; a launch of the persistent kernel costs more than this
@@ -1607,6 +1772,9 @@ struct Lower {
         switch (ch.kind) {
         case CK_SINGLE:
             st = f32 ? lower_f32_single(ci, ch.nodes[0]) : lower_bf16_single(ci, ch.nodes[0]);
+            break;
+        case CK_NORM_QMATMUL:
+            st = lower_qmatmul(ci, ch.nodes[0], ch.nodes[1]);
             break;
         case CK_CONV_CONV_POOL:
             st = lower_f32_linked(ci);
@@ -1704,6 +1872,7 @@ xenos_status_t plan_workspace(Graph &g) {
         touch(L.out, li, true);
         touch(L.in0, li, false); touch(L.in1, li, false); touch(L.in2, li, false); touch(L.skip, li, false);
         touch(L.seg[0].tensor, li, false); touch(L.seg[1].tensor, li, false);
+        for (int t : L.outx) touch(t, li, true);
     }
     size_t off = align_up(g.param_blob.size(), 256);
     g.status_off = off;
@@ -1720,6 +1889,14 @@ xenos_status_t plan_workspace(Graph &g) {
             g.cnt_bytes += align_up((size_t)g.max_batch * L.n_tiles * 8, 16);   // one counter per (image, channel tile)
             g.split_bytes = std::max(g.split_bytes, (size_t)g.max_batch * L.gap_parts * L.npad * 4);
         }
+    for (Launch &L : g.launches) {
+        // 8-bit rows with their scales, parts of rows of scores: in the same region, whose users follow one another
+        g.split_bytes = std::max(g.split_bytes, L.scratch_bytes);
+        if (L.lp_parts_max > 1) {                                                // [arrived] per row that has several parts
+            L.split_cnt_off = off + g.cnt_bytes;
+            g.cnt_bytes += align_up((size_t)2 * g.hw.sm_count * 4, 16);
+        }
+    }
     g.cnt_bytes = align_up(g.cnt_bytes, 256);
     off += g.cnt_bytes;
     g.act_off = off;
@@ -1733,7 +1910,7 @@ xenos_status_t plan_workspace(Graph &g) {
         TensorPlace &p = g.place[t];
         const Tensor &x = g.tensors[t];
         if (f32) { p.dtype = XENOS_DTYPE_F32; p.layout = XENOS_LAYOUT_NCHW; }
-        else { p.dtype = XENOS_DTYPE_BF16; p.layout = XENOS_LAYOUT_NHWC; }
+        else { p.dtype = x.input_slot >= 0 || x.output_slot >= 0 ? XENOS_DTYPE_BF16 : elem_dtype(g, t); p.layout = XENOS_LAYOUT_NHWC; }
         if (x.input_slot >= 0 || x.output_slot >= 0) {
             p.external = true;
             p.dtype = x.io_dtype; p.layout = x.io_layout;
@@ -1789,15 +1966,15 @@ static std::string kernel_of(const Launch &L) {
     static const char *k[] = {"?", "gemm_chain_kernel", "dw3x3_kernel", "pool_kernel", "gap_kernel", "add_kernel", "concat_part_kernel", "mulmac_kernel",
                               "transpose_kernel", "slice_kernel", "f32_conv_kernel", "f32_pool_kernel", "f32_gap_kernel", "f32_add_kernel",
                               "f32_concat_part_kernel", "f32_fc_kernel", "f32_chain_kernel", "f32_mulmac_kernel", "transpose_kernel", "f32_slice_kernel",
-                              "chain2_kernel", "stem3x3_kernel"};
+                              "chain2_kernel", "stem3x3_kernel", "row_kernel", "q8_tc_kernel", "q8_small_kernel", "logprob_kernel"};
     return k[L.kind];
 }
 
 void emit_plan_json(Graph &g) {
-    static const char *nk[] = {"?", "conv", "dwconv", "fc", "maxpool", "avgpool", "gap", "add", "concat", "mul", "mac", "transpose", "split"};
-    static const char *ck[] = {"single", "conv_conv_pool", "dw_pw", "conv_tail", "expand_concat", "matmul_matmul", "conv_conv"};
+    static const char *nk[] = {"?", "conv", "dwconv", "fc", "maxpool", "avgpool", "gap", "add", "concat", "mul", "mac", "transpose", "split", "layernorm", "qmatmul", "logprob"};
+    static const char *ck[] = {"single", "conv_conv_pool", "dw_pw", "conv_tail", "expand_concat", "matmul_matmul", "conv_conv", "norm_qmatmul"};
     static const char *lk[] = {"?", "gemm", "dw", "pool", "gap", "add", "concat_part", "mulmac", "transpose", "slice", "f32_conv", "f32_pool",
-                               "f32_gap", "f32_add", "f32_concat_part", "f32_fc", "f32_conv_conv_pool", "f32_mulmac", "f32_transpose", "f32_slice", "gemm2", "stem3x3"};
+                               "f32_gap", "f32_add", "f32_concat_part", "f32_fc", "f32_conv_conv_pool", "f32_mulmac", "f32_transpose", "f32_slice", "gemm2", "stem3x3", "rows", "q8", "q8_small", "logprob"};
     static const char *am[] = {"none", "gather", "stem", "dw"};
     std::string s = "{";
     jstr(s, "precision", g.precision == XENOS_PRECISION_FP32_CUDA_CORE ? "fp32_cuda_core" : "bf16_tensor");
@@ -1859,6 +2036,15 @@ void emit_plan_json(Graph &g) {
             jint(s, "tile_n", L.tile_n); jint(s, "n_tiles", L.n_tiles); jint(s, "m_tiles", L.m_tiles); jint(s, "npad", L.npad);
             jint(s, "patch_rh", L.patch_rh); jint(s, "patch_rw", L.patch_rw); jint(s, "rh2", L.rh2); jint(s, "rw2", L.rw2);
             jint(s, "tiles_y", L.tiles_y); jint(s, "tiles_x", L.tiles_x); jint(s, "stages", L.stages); jint(s, "b_resident", L.b_resident);
+        }
+        if (L.kind == LK_ROWS) {
+            jint(s, "norm", L.row_norm); jstr(s, "leaves", L.row_out == 2 ? "q8" : L.row_out == 1 ? "f32" : "bf16"); jint(s, "pitch", L.q_pitch);
+        }
+        if (L.kind == LK_Q8 || L.kind == LK_Q8_SMALL) {
+            jint(s, "kblocks", L.kblocks); jint(s, "pitch", L.q_pitch); jint(s, "tile_n", L.tile_n); jint(s, "pair", L.q8_pair); jint(s, "out_dtype", L.out_dtype);
+        }
+        if (L.kind == LK_LOGPROB) {
+            jint(s, "labels", L.n_labels); jint(s, "top", L.top); jarr(s, "outs", std::vector<int>(L.outx, L.outx + 4));
         }
         if (L.kind == LK_F32_CONV_CONV_POOL) {
             jint(s, "parts_outc", L.parts_outc); jint(s, "tile_h", L.tile_h); jint(s, "tile_w", L.tile_w);

@@ -21,7 +21,10 @@
 #include "graph.hpp"
 #include "kernels_bf16.cuh"
 #include "kernels_f32.cuh"
+#include "logprob.cuh"
 #include "pair_tc.cuh"
+#include "q8_tc.cuh"
+#include "rows.cuh"
 
 namespace xenos {
 
@@ -63,6 +66,11 @@ static uint32_t make_idesc(int tile_n) {
     d |= (uint32_t)(tile_n >> 3) << 17; // N / 8
     d |= (uint32_t)(128 >> 4) << 24;    // M / 16
     return d;
+}
+
+static uint32_t make_q8_idesc(int m, int n) {
+    // kind::i8: int32 accumulator, signed 8-bit A and B, both K-major
+    return 2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
 
 // 4-D map (C, W, H, N) over the NHWC bf16 input of a linked depthwise stage; box = one halo tile.
@@ -164,7 +172,47 @@ static bool conv_has_external(const Graph &g, const Launch &L) {
 static bool touches_caller(const Graph &g, const Launch &L) {
     auto external = [&](int t) { return t >= 0 && (g.tensors[t].input_slot >= 0 || g.tensors[t].output_slot >= 0); };
     return external(L.in0) || external(L.in1) || external(L.in2) || external(L.out) || external(L.skip) ||
-           (L.seg[0].mode != AM_NONE && external(L.seg[0].tensor)) || (L.seg[1].mode != AM_NONE && external(L.seg[1].tensor));
+           (L.seg[0].mode != AM_NONE && external(L.seg[0].tensor)) || (L.seg[1].mode != AM_NONE && external(L.seg[1].tensor)) ||
+           external(L.outx[0]) || external(L.outx[1]) || external(L.outx[2]) || external(L.outx[3]);
+}
+
+// Operand of the 8-bit product: rows of `pitch` bytes in boxes of 128 bytes x box_rows, 128-byte swizzle.
+static xenos_status_t encode_bytes_map(const Graph &g, Runtime *rt, void *base, int pitch, long long rows, int box_rows, CUtensorMap *out) {
+    cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)pitch};
+    cuuint32_t box[2] = {128u, (cuuint32_t)box_rows};
+    cuuint32_t estr[2] = {1u, 1u};
+    if (((uintptr_t)base & 15u) || pitch % 128 || box_rows > 256) return fail(g, XENOS_E_CUDA, "internal: an 8-bit matrix is not addressable by TMA");
+    CUresult r = rt->encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(g, XENOS_E_CUDA, "cuTensorMapEncodeTiled (8-bit rows) failed with code " + std::to_string((int)r));
+    return XENOS_OK;
+}
+
+// Layer norm / rounding of rows: the smallest group and number of chunks that hold `n` channels (rows_short), or the walk over memory.
+using RowKernel = void (*)(xk::RowParams);
+struct RowChoice { RowKernel kernel; int threads, rows; };
+template <int G, int V, bool kIn32, int kOut, bool kNorm, bool kVec>
+static RowChoice row_choice() { return {xk::row_kernel<G, V, kIn32, kOut, kNorm, kVec>, xk::RowShape<G, V>::threads, xk::RowShape<G, V>::rows}; }
+template <bool kIn32, int kOut, bool kNorm>
+static RowChoice row_choice(int n, bool vec) {
+    if (n > 16384) return {xk::row_long_kernel<kIn32, kOut, kNorm>, 512, 1};
+    if (!vec)
+        return n <= 128 ? row_choice<8, 2, kIn32, kOut, kNorm, false>() : n <= 1024 ? row_choice<32, 4, kIn32, kOut, kNorm, false>()
+             : n <= 4096 ? row_choice<128, 4, kIn32, kOut, kNorm, false>() : row_choice<512, 4, kIn32, kOut, kNorm, false>();
+    return n <= 64 ? row_choice<8, 1, kIn32, kOut, kNorm, true>() : n <= 128 ? row_choice<8, 2, kIn32, kOut, kNorm, true>()
+         : n <= 256 ? row_choice<32, 1, kIn32, kOut, kNorm, true>() : n <= 512 ? row_choice<32, 2, kIn32, kOut, kNorm, true>()
+         : n <= 1024 ? row_choice<32, 4, kIn32, kOut, kNorm, true>() : n <= 2048 ? row_choice<128, 2, kIn32, kOut, kNorm, true>()
+         : n <= 4096 ? row_choice<128, 4, kIn32, kOut, kNorm, true>() : n <= 8192 ? row_choice<256, 4, kIn32, kOut, kNorm, true>()
+         : row_choice<512, 4, kIn32, kOut, kNorm, true>();
+}
+template <bool kIn32>
+static RowChoice row_choice(const Launch &L) {
+    const int n = L.row_out == xk::RO_Q8 ? L.q_pitch : L.C;
+    const bool vec = L.C % 8 == 0;
+    if (!L.row_norm) return row_choice<kIn32, xk::RO_Q8, false>(n, vec);
+    return L.row_out == xk::RO_Q8 ? row_choice<kIn32, xk::RO_Q8, true>(n, vec) : L.row_out == xk::RO_F32 ? row_choice<kIn32, xk::RO_F32, true>(n, vec)
+                                                                                 : row_choice<kIn32, xk::RO_BF16, true>(n, vec);
 }
 
 static xk::ConvSegment conv_segment(const Launch &L, const ASeg &a) {
@@ -376,6 +424,7 @@ static xenos_status_t attach(Graph &g, void *ws, void *stream_v) {
     int max_gemm_smem = 0, max_chain_smem = 0;
     for (const Launch &L : g.launches) {
         if (L.kind == LK_GEMM2) { any_gemm = true; max_gemm_smem = std::max(max_gemm_smem, L.smem_bytes); }
+        if (L.kind == LK_Q8) { any_gemm = true; max_gemm_smem = std::max(max_gemm_smem, L.smem_bytes); }
         if (L.kind == LK_GEMM) { any_gemm = true; max_gemm_smem = std::max(max_gemm_smem, L.smem_bytes); }
         if (L.kind == LK_F32_CONV_CONV_POOL) {
             max_chain_smem = std::max(max_chain_smem, L.smem_bytes);
@@ -414,6 +463,17 @@ static xenos_status_t attach(Graph &g, void *ws, void *stream_v) {
                 if (st == XENOS_OK) st = encode_weight_map(g, rt, static_cast<uint8_t *>(ws) + L.w2_off, L.kblocks2 * 64, L.npad, L.tile_n, &rt->tmaps2[i]);
                 if (st == XENOS_OK && g.tensors[L.in0].input_slot < 0)
                     st = encode_chain2_input(g, rt, L, static_cast<uint8_t *>(ws) + g.place[L.in0].off, g.max_batch, &rt->hmaps[i]);
+                if (st != XENOS_OK) return st;
+                continue;
+            }
+            if (L.kind == LK_Q8) {
+                // activation rows in the split scratch; weights in boxes of 32, 64 and 128 channels, for the tile widths that runs choose
+                const long long rows = (long long)g.max_batch * L.rows_per_image;
+                uint8_t *w = static_cast<uint8_t *>(ws) + L.w_off;
+                xenos_status_t st = encode_bytes_map(g, rt, static_cast<uint8_t *>(ws) + g.split_off, L.q_pitch, rows, 128, &rt->tmaps[i]);
+                if (st == XENOS_OK) st = encode_bytes_map(g, rt, w, L.q_pitch, L.K, 32, &rt->conv[i].a0);
+                if (st == XENOS_OK) st = encode_bytes_map(g, rt, w, L.q_pitch, L.K, 64, &rt->conv[i].a1);
+                if (st == XENOS_OK) st = encode_bytes_map(g, rt, w, L.q_pitch, L.K, 128, &rt->conv[i].o);
                 if (st != XENOS_OK) return st;
                 continue;
             }
@@ -601,6 +661,70 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
         case LK_F32_SLICE: {
             long long total = (long long)N * L.K * L.H * L.W;
             le = to.plain(xk::f32_slice_kernel, ew_grid(total, 256, sms), 256, 0, (const float *)ptr(L.in0), (float *)ptr(L.out), N, L.K, L.H * L.W, L.C, L.out_coff);
+            break;
+        }
+        case LK_ROWS: {
+            xk::RowParams p;
+            uint8_t *scratch = ws + g.split_off;
+            p.x = ptr(L.in0); p.gamma = (const float *)(ws + L.w_off); p.beta = (const float *)(ws + L.b_off);
+            p.y = L.row_out == xk::RO_Q8 ? scratch : ptr(L.out);
+            p.scale = (float *)(scratch + L.q_scale_off);
+            p.rows = (long long)N * L.rows_per_image; p.C = L.C; p.pitch = L.row_out == xk::RO_Q8 ? L.q_pitch : L.C; p.eps = L.eps;
+            const RowChoice k = L.row_in_f32 ? row_choice<true>(L) : row_choice<false>(L);
+            le = to.pdl(k.kernel, (unsigned)((p.rows + k.rows - 1) / k.rows), k.threads, 0, p);
+            break;
+        }
+        case LK_Q8: {
+            xk::Q8Params p;
+            std::memset(&p, 0, sizeof p);
+            const bool pair = L.q8_pair;
+            p.M = N * L.rows_per_image; p.N = L.K; p.kblocks = L.kblocks;
+            p.tile_n = pair ? 256 : q8_tile_n(g.hw, p.M, p.N, p.kblocks, sms);
+            p.m_tiles = pair ? (p.M + 255) / 256 : (p.M + 127) / 128; p.n_tiles = (p.N + p.tile_n - 1) / p.tile_n;
+            p.xs = (const float *)(ws + g.split_off + L.q_scale_off); p.ws = (const float *)(ws + L.w2_off); p.bias = (const float *)(ws + L.b_off);
+            p.y = ptr(L.out); p.status = status; p.act = L.act; p.out_f32 = L.out_dtype == XENOS_DTYPE_F32; p.vec = L.K % (p.out_f32 ? 4 : 8) == 0;
+            p.stages = q8_stages(g.hw, p.tile_n, pair); p.stage_bytes = q8_stage_bytes(p.tile_n, pair); p.tmem_cols = std::max(32, 2 * p.tile_n);
+            p.off_stage = p.stages * p.stage_bytes; p.off_par = p.off_stage + 8 * 4096; p.off_bar = p.off_par + 8 * 256;
+            p.idesc = make_q8_idesc(pair ? 256 : 128, p.tile_n);
+            p.launch_id = (int)li;
+            const ConvMaps &b = rt->conv[li];
+            const CUtensorMap &tmB = p.tile_n == 32 ? b.a0 : p.tile_n == 64 ? b.a1 : b.o;
+            const int tiles = p.m_tiles * p.n_tiles, smem = q8_smem_bytes(g.hw, p.tile_n, pair);
+            if (pair) le = to.pdl_cluster(xk::q8_tc_kernel<2>, 2 * std::min(tiles, std::max(1, sms / 2)), xk::kQ8Threads, smem, 2, rt->tmaps[li], tmB, p);
+            else le = to.pdl(xk::q8_tc_kernel<1>, std::min(tiles, sms), xk::kQ8Threads, smem, rt->tmaps[li], tmB, p);
+            break;
+        }
+        case LK_Q8_SMALL: {
+            xk::Q8SmallParams p;
+            p.x = ptr(L.in0); p.w = ws + L.w_off; p.ws = (const float *)(ws + L.w2_off); p.bias = (const float *)(ws + L.b_off); p.y = ptr(L.out);
+            p.M = N * L.rows_per_image; p.N = L.K; p.K = L.C; p.pitch = L.q_pitch; p.act = L.act; p.out_f32 = L.out_dtype == XENOS_DTYPE_F32;
+            p.vec = L.C % (L.row_in_f32 ? 4 : 8) == 0;
+            const int grid = (L.K + 15) / 16;
+            if (L.row_in_f32) le = to.pdl(p.M <= 8 ? xk::q8_small_kernel<1, true> : xk::q8_small_kernel<2, true>, grid, 256, 0, p);
+            else le = to.pdl(p.M <= 8 ? xk::q8_small_kernel<1, false> : xk::q8_small_kernel<2, false>, grid, 256, 0, p);
+            break;
+        }
+        case LK_LOGPROB: {
+            xk::LogprobParams p;
+            p.x = ptr(L.in0); p.labels = (const int *)ptr(L.labels);
+            p.lp = (float *)ptr(L.outx[0]); p.entropy = (float *)ptr(L.outx[1]); p.top_id = (int *)ptr(L.outx[2]); p.top_lp = (float *)ptr(L.outx[3]);
+            p.status = status;
+            p.rows = (long long)N * L.rows_per_image; p.V = L.C; p.L = L.n_labels; p.k = L.top;
+            const bool f32 = L.row_in_f32;
+            const int per_chunk = f32 ? 4 : 8, max_chunks = (L.C + 2 * per_chunk - 2) / per_chunk;      // (a row may start inside a chunk)
+            p.parts = 1;
+            if (L.lp_parts_max > 1) {
+                // few rows: CTAs enough for two a unit, each with a chunk for every thread at least
+                const long long fill = 2ll * g.hw.sm_count / p.rows;
+                p.parts = (int)std::max(1ll, std::min(fill, std::min((long long)L.lp_parts_max, (long long)max_chunks / 512)));
+            }
+            p.part_chunks = (max_chunks + p.parts - 1) / p.parts;
+            p.part_mst = (float *)(ws + g.split_off);
+            p.part_key = (unsigned long long *)(ws + g.split_off + (size_t)2 * g.hw.sm_count * 16);
+            p.arrived = (unsigned *)(ws + L.split_cnt_off);
+            if (L.C <= 2048) le = to.pdl(f32 ? xk::logprob_kernel<32, true> : xk::logprob_kernel<32, false>, (unsigned)((p.rows + 7) / 8), 256, 0, p);
+            else if (L.C <= kLpCtaEntries) le = to.pdl(f32 ? xk::logprob_kernel<128, true> : xk::logprob_kernel<128, false>, (unsigned)p.rows, 128, 0, p);
+            else le = to.pdl(f32 ? xk::logprob_kernel<512, true> : xk::logprob_kernel<512, false>, (unsigned)(p.rows * p.parts), 512, 0, p);
             break;
         }
         case LK_GEMM2: {

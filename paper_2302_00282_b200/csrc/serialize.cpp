@@ -8,6 +8,7 @@
 // Layout (little-endian): "XENOSIMG" | u32 version | body | u64 FNV-1a of everything before it.
 // The body is a sequence of i32 / u64 / f32-array fields in the order written below; every count and index is
 // range-checked on load.
+#include <algorithm>
 #include <cstring>
 #include <string>
 #include <vector>
@@ -19,7 +20,7 @@ namespace xenos {
 namespace {
 
 constexpr char kMagic[8] = {'X', 'E', 'N', 'O', 'S', 'I', 'M', 'G'};
-constexpr uint32_t kVersion = 1;
+constexpr uint32_t kVersion = 2;      // 1: before the row operators; graphs without them are still written so
 
 uint64_t fnv1a(const uint8_t *p, size_t n) {
     uint64_t h = 1469598103934665603ull;
@@ -65,7 +66,10 @@ struct Reader {
 void save_graph(const Graph &g, std::vector<uint8_t> &out) {
     Writer w;
     w.raw(kMagic, 8);
-    w.raw(&kVersion, 4);
+    bool rows = false;
+    for (const Op &o : g.ops) rows = rows || o.kind >= XENOS_OP_LAYERNORM;
+    const uint32_t version = rows ? kVersion : 1u;
+    w.raw(&version, 4);
     w.i32(g.hw.sm_count); w.i32(g.hw.smem_bytes_per_cta); w.i32(g.hw.tmem_columns); w.u64((uint64_t)g.hw.l2_bytes);
     w.u64(g.tensors.size());
     for (const Tensor &t : g.tensors) {
@@ -78,6 +82,11 @@ void save_graph(const Graph &g, std::vector<uint8_t> &out) {
         w.ints(o.in); w.i32(o.out);
         w.floats(o.w); w.floats(o.bias); w.floats(o.gamma); w.floats(o.beta); w.floats(o.mean); w.floats(o.var);
         w.f32(o.eps); w.i32(o.has_bias); w.i32(o.has_bn);
+        if (version < 2) continue;
+        w.u64(o.q.size());
+        if (!o.q.empty()) w.raw(o.q.data(), o.q.size());
+        w.i32(o.top);
+        for (int t : o.outs) w.i32(t);
     }
     w.ints(g.inputs); w.ints(g.outputs);
     w.i32(g.link_auto);
@@ -105,7 +114,7 @@ xenos_status_t load_graph(Graph &g, const uint8_t *buf, size_t bytes, bool *comp
     r.at = 8;
     uint32_t ver = 0;
     r.take(&ver, 4);
-    if (ver != kVersion) return fail(g, XENOS_E_INVALID, "load: image version " + std::to_string(ver) + " is not supported");
+    if (ver != 1 && ver != kVersion) return fail(g, XENOS_E_INVALID, "load: image version " + std::to_string(ver) + " is not supported");
     g.hw.sm_count = r.i32(); g.hw.smem_bytes_per_cta = r.i32(); g.hw.tmem_columns = r.i32(); g.hw.l2_bytes = (int64_t)r.u64();
     if (g.hw.sm_count < 1 || g.hw.smem_bytes_per_cta < 48 * 1024 || g.hw.tmem_columns < 32 || g.hw.tmem_columns > 512 || g.hw.l2_bytes < 0)
         return fail(g, XENOS_E_INVALID, "load: hardware info out of range");
@@ -122,6 +131,11 @@ xenos_status_t load_graph(Graph &g, const uint8_t *buf, size_t bytes, bool *comp
         o.in = r.ints(); o.out = r.i32();
         o.w = r.floats(); o.bias = r.floats(); o.gamma = r.floats(); o.beta = r.floats(); o.mean = r.floats(); o.var = r.floats();
         o.eps = r.f32(); o.has_bias = r.i32() != 0; o.has_bn = r.i32() != 0;
+        if (ver < 2) continue;
+        o.q.resize(r.count(1));
+        if (!o.q.empty()) r.take(o.q.data(), o.q.size());
+        o.top = r.i32();
+        for (int &t : o.outs) t = r.i32();
     }
     g.inputs = r.ints(); g.outputs = r.ints();
     g.link_auto = r.i32() != 0;
@@ -150,7 +164,41 @@ xenos_status_t load_graph(Graph &g, const uint8_t *buf, size_t bytes, bool *comp
     for (const Op &o : g.ops) {
         if (!tid(o.out)) return fail(g, XENOS_E_INVALID, "load: operator output out of range");
         for (int x : o.in) if (!tid(x)) return fail(g, XENOS_E_INVALID, "load: operator input out of range");
+        if (o.kind < XENOS_OP_LAYERNORM) continue;
+        // (the lowering of the row operators indexes by these)
+        const char *bad = ver < 2 || o.kind > XENOS_OP_LOGPROB || o.in.empty() ? "kind" : nullptr;
+        if (!bad) {
+            const size_t c = (size_t)g.tensors[o.in[0]].c, n = (size_t)std::max(o.cout, 0);
+            if (o.kind == XENOS_OP_LAYERNORM && (o.w.size() != c || (o.has_bias && o.bias.size() != c) || !(o.eps > 0.0f))) bad = "layernorm";
+            if (o.kind == XENOS_OP_QMATMUL && (!n || c > 131072 || o.q.size() != n * c || o.gamma.size() != n || (o.has_bias && o.bias.size() != n))) bad = "qmatmul";
+            if (o.kind == XENOS_OP_LOGPROB) {
+                if (o.top < 0 || o.top > 32 || o.in.size() > 2 || o.outs[1] != o.out || (o.in.size() == 2) != (o.outs[0] >= 0) || (o.top > 0) != (o.outs[2] >= 0) || (o.top > 0) != (o.outs[3] >= 0)) bad = "logprob";
+                for (int i = 0; i < 4 && !bad; ++i) {
+                    if (o.outs[i] < 0) continue;
+                    if (!tid(o.outs[i])) { bad = "logprob"; break; }
+                    Tensor &y = g.tensors[o.outs[i]];
+                    const Tensor &x = g.tensors[o.in[0]];
+                    if (y.input_slot >= 0 || y.h != x.h || y.w != x.w || y.is_vec != x.is_vec || y.c != (i == 0 ? g.tensors[o.in[1]].c : i == 1 ? 1 : o.top)) bad = "logprob";
+                    y.fixed = i == 2 ? XENOS_DTYPE_I32 : XENOS_DTYPE_F32;
+                }
+                if (!bad && o.in.size() == 2) {
+                    const Tensor &l = g.tensors[o.in[1]], &x = g.tensors[o.in[0]];
+                    if (l.input_slot < 0 || l.io_dtype != XENOS_DTYPE_I32 || l.rows() != x.rows()) bad = "logprob";
+                }
+            }
+        }
+        if (bad) return fail(g, XENOS_E_INVALID, std::string("load: a row operator's fields do not fit (") + bad + ")");
     }
+    bool any_rows = false;
+    for (const Op &o : g.ops) {
+        any_rows = any_rows || o.kind >= XENOS_OP_LAYERNORM;
+        for (size_t i = 0; i < o.in.size(); ++i) {
+            const Tensor &x = g.tensors[o.in[i]];
+            const bool label = o.kind == XENOS_OP_LOGPROB && i == 1;
+            if (x.fixed >= 0 || (!label && x.input_slot >= 0 && x.io_dtype == XENOS_DTYPE_I32)) return fail(g, XENOS_E_INVALID, "load: an operator reads a tensor that cannot be an operand");
+        }
+    }
+    if (any_rows != (ver == kVersion)) return fail(g, XENOS_E_INVALID, "load: the image's version does not go with its operators");
     for (int x : g.inputs) if (!tid(x)) return fail(g, XENOS_E_INVALID, "load: graph input out of range");
     for (int x : g.outputs) if (!tid(x)) return fail(g, XENOS_E_INVALID, "load: graph output out of range");
     for (const LinkRequest &q : g.link_requests) for (int x : q.ops) if (!tid(x)) return fail(g, XENOS_E_INVALID, "load: link request out of range");
