@@ -281,7 +281,7 @@ inline int out_dim(int in, int k, int stride, int pad) {
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 constexpr int kQ8SmallRows = 16;         // rows up to which q8_small_kernel takes an 8-bit product
-constexpr int kLpCtaEntries = 8192;      // entries above which a row of scores has CTAs of 512 threads, and may have several
+constexpr int kLpCtaEntries = 8192;      // entries above which a row of scores may have CTAs of 256 threads, and several of them
 
 // Channel tile of an 8-bit product in tiles of one CTA: modelled cycles.  A block of 128 deep takes the slower of the tensor pipe (2 cycles a
 // column) and the operands' way from L2 (75 bytes a cycle); a tile's fill and epilogue come on top.

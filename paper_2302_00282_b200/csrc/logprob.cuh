@@ -3,17 +3,21 @@
 //   m = max x,  S = sum e^(x - m),  T = sum (x - m) e^(x - m)
 //   log p_i = x_i - m - ln S,   entropy = ln S - T / S,   best: by value, equal values by index
 //
-// Bound by HBM at long rows (one read, next to nothing written).  One pass: a thread keeps its running maximum with S and T relative to
-// it (rescaled when the maximum grows, which happens some ln n times), and the chunk that its maximum came from.
-// The k best come almost free from what the pass leaves: G maxima of threads, in 64 groups (32: lanes of a warp).  The k-th largest
-// group maximum is a lower bound of the k-th best entry, since k groups have an entry at or above it; so only threads whose own maximum
-// reaches it look at their chunks again (from L1 or L2), and put the entries that reach it, some k of them, into a list in
-// shared memory, where an entry's place is the number of entries before it.  A list that overflows (many equal or sorted scores in one
-// thread's chunks) is replaced by k rounds of a maximum below the last one.
+// One pass over a row in 16-byte chunks, four a thread and step, which are on their way to shared memory a step ahead (each thread reads what it
+// asked for itself: no barrier).  A thread keeps its maximum with the step that it came from, and S and T relative to a reference that
+// follows the maximum only when that is more than 20 above it (terms up to e^20 are as good as terms up to 1; a running maximum as reference would
+// be rescaled in every step by one lane of a warp or another).  An entry costs one instruction of the special function unit (16 a
+// cycle and SM) and some five others, two entries per instruction where the fp32 pipe has packed forms.
+// The k best come almost free from what the pass leaves, G maxima of threads: of 32 groups of threads the k-th largest maximum is a lower
+// bound of the k-th best entry, since k groups have an entry at or above it; so only chunks of threads whose own maximum reaches
+// it are looked at again (from L1 or L2, by all threads), and entries that reach it, some k of them, go into a list in shared memory, where an
+// entry's place is the number of entries before it.  A list that overflows (many sorted scores) is replaced by k rounds of a
+// maximum below the last one.
 // Entries are ordered by (value, index), which no two share: results do not depend on the order in which threads reach the list.
 //
-// Rows: up to 2048 entries a warp, up to 8192 128 threads, above 512 threads.  Few long rows are cut over several CTAs (up to 16 a
-// row); each leaves (m, S, T) and its k best in the workspace, the last to arrive joins them in ascending order.
+// A row is a warp's, 128 threads' or 256 threads' (what a row costs beside its entries, some 500 instructions a warp, is the less the fewer
+// warps share it; so the rule is the fewest that keep the SMs busy), and few long rows are cut over several CTAs (up to 16 a row): each leaves (m, S, T) and its
+// k best in the workspace, the last to arrive joins them.
 #pragma once
 
 #include "rows.cuh"
@@ -58,25 +62,59 @@ __device__ __forceinline__ LpSum lp_rebase(const LpSum &a, float to) {
     return a.m > -INFINITY || a.s != 0.0f ? LpSum{to, a.s * f, fmaf(a.s, d, a.t) * f} : LpSum{to, 0.0f, 0.0f};
 }
 
+// Two fp32 values that one instruction works on.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair2(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void split2(f32x2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+
+// Adds 2^d and d 2^d, d = x log2(e) - c, of U chunks.
+template <bool kIn32, int U, bool kMasked>
+__device__ __forceinline__ void lp_add(const uint4 *u, f32x2 l2, f32x2 nc2, f32x2 &s, f32x2 &t) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+#pragma unroll
+        for (int c = 0; c < (kIn32 ? 2 : 4); ++c) {
+            const float lo = kIn32 ? __uint_as_float(w[2 * c % 4]) : __uint_as_float(w[c] << 16);
+            const float hi = kIn32 ? __uint_as_float(w[(2 * c + 1) % 4]) : __uint_as_float(w[c] & 0xffff0000u);
+            f32x2 d = fma2(pair2(lo, hi), l2, nc2);
+            float da, db;
+            split2(d, da, db);
+            if (kMasked) { da = max_nan(da, -300.0f); db = max_nan(db, -300.0f); d = pair2(da, db); }
+            const f32x2 e = pair2(ex2(da), ex2(db));
+            s = add2(s, e);
+            t = fma2(d, e, t);
+        }
+    }
+}
+
 template <int G> struct LpShape {
-    static constexpr int threads = G == 32 ? 256 : G;
+    static constexpr int threads = G == 32 ? 128 : G;
+    static constexpr int resident = 1024 / threads;     // CTAs per SM that the registers are for
     static constexpr int rows = threads / G;
-    static constexpr int groups = G == 32 ? 32 : 64;
     static constexpr int cap = G == 32 ? 256 : 512;
     static constexpr int warps = G / 32;
+    static constexpr int ahead = 1;                        // steps under way beside the one at hand
 };
 template <int G>
 struct LpShared {
+    __align__(16) uint32_t value[32];          // (read 16 bytes at a time)
     LpKey list[LpShape<G>::cap];
     LpKey best[kLpMaxTop];
     LpKey key[G == 32 ? 1 : G];
-    LpKey group[G == 32 ? 1 : 64];
-    LpKey floor;
+    uint32_t floor;
+    int floor_at;
     LpSum sum[LpShape<G>::warps];
     float mx[LpShape<G>::warps];
     LpKey mk[LpShape<G>::warps];
-    int n, last;
+    unsigned short who[G];         // threads whose chunks are looked at again
+    int n, nwho, last;
 };
+static_assert(sizeof(LpShared<32>) % 16 == 0 && sizeof(LpShared<128>) % 16 == 0 && sizeof(LpShared<256>) % 16 == 0, "value must stay aligned in an array");
 template <int G> __device__ __forceinline__ void lp_sync() { if (G == 32) __syncwarp(); else __syncthreads(); }
 
 // A row's chunks as aligned 16-byte pieces: chunk j holds entries [j * E - lead, ...) of the row; pieces that reach over
@@ -111,20 +149,33 @@ struct LpRow {
         if (whole(j)) unpack(*reinterpret_cast<const uint4 *>(base + (size_t)j * 16), v);
         else edge(j, v);
     }
+    // The bits of a chunk at a row's end or behind it, -inf for what is not the row's.
+    __device__ __forceinline__ uint4 cut(int j, int end) const {
+        constexpr uint32_t none = kIn32 ? 0xff800000u : 0xff80ff80u;
+        uint4 u = make_uint4(none, none, none, none);
+        if (j < end) {
+            float v[E];
+            edge(j, v);
+            u = kIn32 ? make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]))
+                      : make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4 % E], v[5 % E]), pack2(v[6 % E], v[7 % E]));
+        }
+        return u;
+    }
     __device__ __forceinline__ float entry(int e) const {
         return kIn32 ? reinterpret_cast<const float *>(base)[e + lead] : __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(base)[e + lead]);
     }
 };
 
-// Results of a row from its sums and its best entries in order.
+// Results of a row from its sums and its best entries in order.  lab0, x0: the thread's first label and its score.
 template <int G, bool kIn32>
-__device__ __forceinline__ void lp_finish(const LogprobParams &p, const LpRow<kIn32> &x, long long row, int t, const LpSum &a, const LpKey *best) {
+__device__ __forceinline__ void lp_finish(const LogprobParams &p, const LpRow<kIn32> &x, long long row, int t, const LpSum &a, const LpKey *best, int lab0, float x0) {
+    if (t >= 32) return;
     const bool empty = !(a.m > -INFINITY) && a.s == 0.0f;
     const float m = empty ? 0.0f : a.m, ls = empty ? 0.0f : logf(a.s);
-    for (int l = t; p.lp && l < p.L; l += G) {
-        const int lab = p.labels[row * p.L + l];
+    for (int l = t; p.lp && l < p.L; l += 32) {
+        const int lab = l == t ? lab0 : p.labels[row * p.L + l];
         float r = 0.0f;
-        if (lab >= 0 && lab < p.V) r = (x.entry(lab) - m) - ls;
+        if (lab >= 0 && lab < p.V) r = ((l == t ? x0 : x.entry(lab)) - m) - ls;
         else if (lab != -1) {
             r = __uint_as_float(0x7fc00000u);
             atomicCAS(p.status, 0u, kStatusBounds);
@@ -132,83 +183,174 @@ __device__ __forceinline__ void lp_finish(const LogprobParams &p, const LpRow<kI
         p.lp[row * p.L + l] = r;
     }
     if (p.entropy && t == 0) p.entropy[row] = empty ? 0.0f : ls - a.t / a.s;
-    for (int i = t; i < p.k; i += G) {
+    if (t < p.k) {
+        const int i = t;
         const LpKey key = best[i];
         if (p.top_id) p.top_id[row * p.k + i] = key ? (int)~(uint32_t)key : -1;
         if (p.top_lp) p.top_lp[row * p.k + i] = key ? (lp_value((uint32_t)(key >> 32)) - m) - ls : a.s == a.s ? -INFINITY : a.s;
     }
 }
 
-// Places of the n listed keys; the first k go to best (which holds zeros).
+// Places of the n listed keys; the first k go to best (which holds zeros).  Four lanes compare a key with a quarter of the others each.
 template <int G>
 __device__ __forceinline__ void lp_rank(const LpKey *list, int n, int k, LpKey *best, int t) {
-    for (int c = t; c < n; c += G) {
-        const LpKey mine = list[c];
+    for (int c0 = 0; c0 < n; c0 += G / 4) {
+        const int c = c0 + (t >> 2);
+        const LpKey mine = c < n ? list[c] : 0ull;
         int before = 0;
-        for (int o = 0; o < n; ++o) before += list[o] > mine;
-        if (before < k && mine) best[before] = mine;
+#pragma unroll 4
+        for (int o = t & 3; o < n; o += 4) before += list[o] > mine;
+        before += __shfl_xor_sync(0xffffffffu, before, 1);
+        before += __shfl_xor_sync(0xffffffffu, before, 2);
+        if ((t & 3) == 0 && before < k && mine) best[before] = mine;
     }
 }
 
 template <int G, bool kIn32>
-__global__ void __launch_bounds__(LpShape<G>::threads)
+__global__ void __launch_bounds__(LpShape<G>::threads, LpShape<G>::resident)
 logprob_kernel(const LogprobParams p) {
     typedef LpShape<G> Shape;
     constexpr int E = LpRow<kIn32>::E, U = 4;
     constexpr float log2e = 1.44269504f;
     __shared__ LpShared<G> shared[Shape::rows];
+    __shared__ uint4 ring[Shape::ahead + 1][U][Shape::threads];
     LpShared<G> &sh = shared[threadIdx.x / G];
     pdl_launch_dependents();
     pdl_wait();
     const int t = threadIdx.x % G;
-    const int part = G == 512 ? (int)(blockIdx.x % p.parts) : 0;
-    const long long row = G == 512 ? (long long)(blockIdx.x / p.parts) : (long long)blockIdx.x * Shape::rows + threadIdx.x / G;
+    const int part = G == 256 ? (int)(blockIdx.x % p.parts) : 0;
+    const long long row = G == 256 ? (long long)(blockIdx.x / p.parts) : (long long)blockIdx.x * Shape::rows + threadIdx.x / G;
     if (row >= p.rows) return;
     LpRow<kIn32> x;
     x.init(p.x, row, p.V);
-    const int c0 = G == 512 ? part * p.part_chunks : 0, c1 = G == 512 ? min(x.chunks, c0 + p.part_chunks) : x.chunks;
+    const int c0 = G == 256 ? part * p.part_chunks : 0, c1 = G == 256 ? min(x.chunks, c0 + p.part_chunks) : x.chunks;
+    int lab0 = -1;
+    if (p.lp && t < p.L && t < 32) lab0 = p.labels[row * p.L + t];
 
-    LpSum a{-INFINITY, 0.0f, 0.0f};
-    float ms = 0.0f;                       // a.m, 0 while that is -inf
-    int jb = 0;
-    auto take = [&](const float *v, int j) {
-        float cm = v[0];
+    // The sums are kept in powers of two: with c = ms log2(e) rounded, a term is 2^(x log2(e) - c), one fused multiply-add and one
+    // instruction; what c is off by is known (a fused multiply-add gives it) and taken back at the end.
+    float m = -INFINITY, ms = 0.0f, above = -INFINITY;      // the thread's maximum, the sums' reference and what makes that follow
+    int jb = 0;                                             // first chunk of the step with the maximum
+    f32x2 s2 = 0ull, t2 = 0ull, nc2 = 0ull;                 // sums of terms, of terms times exponents; -c
+    const f32x2 l2 = pair2(log2e, log2e);
+    bool masked = false;
+    // 16 or 32 entries: their maximum first, then two by two
+    auto take = [&](const uint4 *u, int j, bool cut) {
+        float gm;
+        if (kIn32) {
+            gm = -INFINITY;
 #pragma unroll
-        for (int i = 1; i < E; ++i) cm = fmaxf(cm, v[i]);
-        if (cm > a.m) {
-            if (a.s != 0.0f) a = lp_rebase(a, cm);
-            a.m = ms = cm; jb = j;
+            for (int i = 0; i < U; ++i)
+                gm = fmaxf(fmaxf(fmaxf(__uint_as_float(u[i].x), __uint_as_float(u[i].y)), fmaxf(__uint_as_float(u[i].z), __uint_as_float(u[i].w))), gm);
+        } else {
+            uint32_t w = 0xff80ff80u;
+#pragma unroll
+            for (int i = 0; i < U; ++i) w = max_bf16x2(max_bf16x2(max_bf16x2(u[i].x, u[i].y), max_bf16x2(u[i].z, u[i].w)), w);
+            gm = fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
         }
+        jb = gm > m ? j : jb;
+        m = fmaxf(m, gm);
+        if (gm > above) {
+            const float c = gm * log2e;
+            if (above > -INFINITY) {       // (before the first finite entry the sums are 0, or NaN)
+                float old, same;
+                split2(nc2, old, same);
+                const float d = fmaxf(-old - c, -1e4f), f = ex2(d);
+                const f32x2 f2 = pair2(f, f);
+                t2 = mul2(fma2(s2, pair2(d, d), t2), f2); s2 = mul2(s2, f2);
+            }
+            ms = gm; above = gm + 20.0f;
+            nc2 = pair2(-c, -c);
+        }
+        if (!(fabsf(ms) < 1e37f)) {        // (such a reference leaves the range when multiplied: differences first)
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const float d = v[i] - ms, e = ex2(d * log2e);
-            a.s += e;
-            a.t = fmaf(fmaxf(d, -200.0f), e, a.t);        // (e is 0 there; -inf * 0 would not be)
+            for (int i = 0; i < U; ++i) {      // (unrolled: a run-time index would put the entries into local memory in every step)
+                float v[E], s = 0.0f, q = 0.0f;
+                x.unpack(u[i], v);
+#pragma unroll
+                for (int c = 0; c < E; ++c) {
+                    const float d = (v[c] - ms) * log2e, e = ex2(d);
+                    s += e;
+                    q = fmaf(fmaxf(d, -300.0f), e, q);
+                }
+                s2 = add2(s2, pair2(s, 0.0f)); t2 = add2(t2, pair2(q, 0.0f));
+            }
+        }
+        const bool near = fabsf(ms) < 1e37f;
+        // Masked entries (-inf, or so low that the exponent leaves the range) have the term 0, and -inf * 0 is NaN.  A warp that meets one adds
+        // the step again with no exponent below -300, and goes on so (a fifth more instructions);
+        // steps with places behind the row's end (cut) are added that way.
+        if (!masked && !cut) {
+            f32x2 sn = s2, tn = t2;
+            lp_add<kIn32, U, false>(u, l2, nc2, sn, tn);
+            float ta, tb;
+            split2(tn, ta, tb);
+            masked = __any_sync(0xffffffffu, near && !(ta + tb == ta + tb));
+            if (!masked && near) { s2 = sn; t2 = tn; }
+        }
+        if (masked || cut) {
+            f32x2 sn = s2, tn = t2;
+            lp_add<kIn32, U, true>(u, l2, nc2, sn, tn);
+            if (near) { s2 = sn; t2 = tn; }
         }
     };
-    int j = c0 + t;
-    if (t == 0 && j < c1 && !x.whole(j)) { float v[E]; x.edge(j, v); take(v, j); j += G; }      // (only a row's first chunk and its last)
-    const int whole1 = c1 == x.chunks && !x.whole(c1 - 1) ? c1 - 1 : c1;
-    for (; j + (U - 1) * G < whole1; j += U * G) {
-        uint4 u[U];
+    const int w0 = x.whole(0) ? 0 : 1, w1 = x.whole(x.chunks - 1) ? c1 : min(c1, x.chunks - 1);
+    // step n of the thread: chunks c0 + t + (n U + i) G, i = 0 .. U - 1
+    constexpr int D = Shape::ahead + 1;
+    const uint32_t slot0 = smem_u32(&ring[0][0][threadIdx.x]);
+    constexpr uint32_t per_chunk = Shape::threads * 16, per_step = U * per_chunk;
+    auto whole_step = [&](int j) { return j >= w0 && j + (U - 1) * G < w1; };
+    auto ask = [&](int j, uint32_t slot) {
+        if (whole_step(j)) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) u[i] = *reinterpret_cast<const uint4 *>(x.base + (size_t)(j + i * G) * 16);
+            for (int i = 0; i < U; ++i) cp_async16(slot + i * per_chunk, x.base + (size_t)(uint32_t)j * 16 + i * G * 16, 16u);
+        } else {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            float v[E];
-            x.unpack(u[i], v);
-            take(v, j + i * G);
+            for (int i = 0; i < U; ++i)
+                if (j + i * G >= w0 && j + i * G < w1) cp_async16(slot + i * per_chunk, x.base + (size_t)(uint32_t)(j + i * G) * 16, 16u);
         }
+        cp_async_commit();
+    };
+    uint32_t put = slot0, get = slot0;
+#pragma unroll
+    for (int n = 0; n < D - 1; ++n) { ask(c0 + t + n * U * G, put); put += per_step; }
+    const int steps = max(0, (c1 - c0 - (t & ~31) + U * G - 1) / (U * G));      // of the warp
+#pragma unroll 1
+    for (int n = 0, j = c0 + t; n < steps; ++n, j += U * G) {
+        if (n + D - 1 < steps) ask(j + (D - 1) * U * G, put);
+        else cp_async_commit();
+        put = put == slot0 + (D - 1) * per_step ? slot0 : put + per_step;
+        cp_async_wait<D - 1>();
+        uint4 u[U];
+        const bool cut = __any_sync(0xffffffffu, !whole_step(j));
+        if (!cut) {
+#pragma unroll
+            for (int i = 0; i < U; ++i) u[i] = ld_shared16(get + i * per_chunk);
+        } else {
+#pragma unroll
+            for (int i = 0; i < U; ++i) u[i] = j + i * G >= w0 && j + i * G < w1 ? ld_shared16(get + i * per_chunk) : x.cut(j + i * G, c1);
+        }
+        get = get == slot0 + (D - 1) * per_step ? slot0 : get + per_step;
+        take(u, j, cut);
     }
-    for (; j < c1; j += G) { float v[E]; x.load(j, v); take(v, j); }
+    float x0 = 0.0f;
+    if (lab0 >= 0 && lab0 < p.V) x0 = x.entry(lab0);
 
     // ---- sums of the group
     const int lane = t & 31, warp = t >> 5;
-    const LpKey mine = (LpKey)lp_order(a.m) << 32 | (uint32_t)~jb;
-    const LpKey key = lp_order(a.m) ? mine : 0ull;
-    float m = a.m;
+    LpSum a;
+    {
+        float sa, sb, ta, tb;
+        split2(s2, sa, sb); split2(t2, ta, tb);
+        // back to natural exponents relative to ms itself
+        const float c = ms * log2e, off = fabsf(ms) < 1e37f ? fmaf(ms, log2e, -c) : 0.0f, f = ex2(-off);
+        a.m = m > -INFINITY ? ms : m; a.s = (sa + sb) * f; a.t = fmaf(-off, sa + sb, ta + tb) * f * 0.693147181f;
+    }
+    const LpKey key = lp_order(m) ? (LpKey)lp_order(m) << 32 | (uint32_t)~jb : 0ull;
 #pragma unroll
     for (int s = 16; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+    if (t < kLpMaxTop) sh.best[t] = 0ull;
+    if (t == 0) { sh.n = 0; sh.nwho = 0; }
     if (G > 32) {
         if (lane == 0) sh.mx[warp] = m;
         sh.key[t] = key;
@@ -217,20 +359,32 @@ logprob_kernel(const LogprobParams p) {
 #pragma unroll
         for (int w = 1; w < Shape::warps; ++w) m = fmaxf(m, sh.mx[w]);
     }
+    // ---- the k-th largest maximum of 32 groups of threads (0: fewer have one)
+    if (p.k && warp == 0) {
+        LpKey g = key;
+        if (G > 32) {
+#pragma unroll
+            for (int i = 32; i < G; i += 32) g = max(g, sh.key[lane + i]);
+        }
+        // A lane's place is the number of larger values (k rounds of a warp-wide maximum take 20 cycles of the SM each).  Equal values count
+        // up to the last step that one of their lanes has it from.
+        const uint32_t o = (uint32_t)(g >> 32);
+        sh.value[lane] = o;
+        __syncwarp();
+        int before = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(&sh.value[4 * i]);
+            before += (q.x > o) + (q.y > o) + (q.z > o) + (q.w > o);
+        }
+        const uint32_t f = __reduce_min_sync(0xffffffffu, before < p.k ? o : 0xffffffffu);
+        const uint32_t at = __reduce_max_sync(0xffffffffu, o == f ? ~(uint32_t)g : 0u);
+        if (lane == 0) { sh.floor = f; sh.floor_at = (int)at; }
+    }
     a = lp_rebase(a, m > -INFINITY ? m : 0.0f);
 #pragma unroll
     for (int s = 16; s >= 1; s >>= 1) { a.s += __shfl_xor_sync(0xffffffffu, a.s, s); a.t += __shfl_xor_sync(0xffffffffu, a.t, s); }
-    if (G > 32) {
-        if (lane == 0) sh.sum[warp] = a;
-        if (t < 64) {
-            LpKey g = sh.key[t];
-#pragma unroll
-            for (int i = 64; i < G; i += 64) g = max(g, sh.key[t + i]);
-            sh.group[t] = g;
-        }
-    }
-    if (t < kLpMaxTop) sh.best[t] = 0ull;
-    if (t == 0) { sh.n = 0; sh.floor = 0ull; }
+    if (G > 32 && lane == 0) sh.sum[warp] = a;
     lp_sync<G>();
     if (G > 32) {
         a = sh.sum[0];
@@ -240,35 +394,43 @@ logprob_kernel(const LogprobParams p) {
     a.m = m;
 
     if (p.k) {
-        // ---- the k-th largest group maximum
-        if (G == 32) {
-            int before = 0;
-#pragma unroll
-            for (int o = 0; o < 32; ++o) before += __shfl_sync(0xffffffffu, key, o) > key;
-            if (before == p.k - 1) sh.floor = key;
-        } else if (t < 64) {
-            const LpKey g = sh.group[t];
-            int before = 0;
-#pragma unroll 8
-            for (int o = 0; o < 64; ++o) before += sh.group[o] > g;
-            if (before == p.k - 1) sh.floor = g;
+        // ---- entries that reach it, among the chunks of the threads whose maximum does
+        const uint32_t fo = sh.floor;
+        const float fv = fo ? lp_value(fo) : -INFINITY;            // (no floor: every entry above -inf counts)
+        // Entries equal to the floor count up to the last chunk of that step: k groups have theirs no later, nor do the maxima of the threads that
+        // hold such entries come later.
+        const int fj = fo ? sh.floor_at + (U - 1) * G : -1;
+        const uint32_t ko = (uint32_t)(key >> 32);
+        const uint32_t reach = __ballot_sync(0xffffffffu, ko > fo || (ko == fo && ko && jb <= fj));
+        if (reach) {
+            int at = 0;
+            if (G > 32 && lane == 0) at = atomicAdd(&sh.nwho, __popc(reach));
+            if (G > 32) at = __shfl_sync(0xffffffffu, at, 0);
+            else if (lane == 0) sh.nwho = __popc(reach);
+            if (reach >> lane & 1u) sh.who[at + __popc(reach & ((1u << lane) - 1u))] = (unsigned short)t;
         }
         lp_sync<G>();
-        const uint32_t fv = (uint32_t)(sh.floor >> 32), fj = ~(uint32_t)sh.floor;       // (no floor: every entry above -inf counts)
-        // ---- entries that reach it
-        if (key && key >= sh.floor)
-            for (int j = c0 + t; j < c1; j += G) {
-                float v[E];
-                x.load(j, v);
+        // (a row of few steps is still in shared memory)
+        const bool kept = (c1 - c0 + U * G - 1) / (U * G) <= D;
+        const int lg = 32 - __clz(max((c1 - c0 + G - 1) / G - 1, 0)), items = sh.nwho << lg;      // chunks of a thread, up to a power of two
+        for (int it = t; it < items; it += G) {
+            const int w = sh.who[it >> lg], n = it & ((1 << lg) - 1), j = c0 + w + n * G;
+            if (j >= c1) continue;
+            float v[E];
+            if (kept && j >= w0 && j < w1) x.unpack(ld_shared16(slot0 + (uint32_t)(w - t) * 16 + (uint32_t)n * per_chunk), v);
+            else x.load(j, v);
+            const float fe = j <= fj ? fv : __uint_as_float(0x7fc00000u);
+            uint32_t hit = 0;
 #pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const uint32_t o = lp_order(v[i]);
-                    if (o > fv || (o == fv && o && (uint32_t)j <= fj)) {
-                        const int at = atomicAdd(&sh.n, 1);
-                        if (at < Shape::cap) sh.list[at] = (LpKey)o << 32 | (uint32_t)~(j * E + i - x.lead);
-                    }
-                }
+            for (int i = 0; i < E; ++i) hit |= v[i] > fv || v[i] == fe ? 1u << i : 0u;
+            for (; hit; hit &= hit - 1) {
+                const int i = __ffs(hit) - 1, at = atomicAdd(&sh.n, 1);
+                float h = v[0];
+#pragma unroll
+                for (int c = 1; c < E; ++c) h = i == c ? v[c] : h;
+                if (at < Shape::cap) sh.list[at] = (LpKey)lp_order(h) << 32 | (uint32_t)~(j * E + i - x.lead);
             }
+        }
         lp_sync<G>();
         if (sh.n <= Shape::cap) lp_rank<G>(sh.list, sh.n, p.k, sh.best, t);
         else {
@@ -303,38 +465,39 @@ logprob_kernel(const LogprobParams p) {
         }
         lp_sync<G>();
     }
-    if (G != 512 || p.parts == 1) {
-        lp_finish<G, kIn32>(p, x, row, t, a, sh.best);
+    if (G != 256 || p.parts == 1) {
+        lp_finish<G, kIn32>(p, x, row, t, a, sh.best, lab0, x0);
         return;
     }
     // ---- a row of several CTAs: leave the part, the last to arrive joins them
     const long long slot = row * p.parts + part;
     if (t == 0) *reinterpret_cast<float4 *>(p.part_mst + slot * 4) = make_float4(a.m, a.s, a.t, 0.0f);
     if (t < p.k) p.part_key[slot * p.k + t] = sh.best[t];
-    __threadfence();
     __syncthreads();
     if (t == 0) {
+        __threadfence();
         sh.last = atomicAdd(p.arrived + row, 1u) == (unsigned)p.parts - 1;
         if (sh.last) p.arrived[row] = 0u;
     }
     __syncthreads();
     if (!sh.last) return;
     __threadfence();
-    LpSum all{-INFINITY, 0.0f, 0.0f};
-    for (int q = 0; q < p.parts; ++q) all.m = fmaxf(all.m, __ldcg(p.part_mst + (row * p.parts + q) * 4));
-    const float to = all.m > -INFINITY ? all.m : 0.0f;
-    for (int q = 0; q < p.parts; ++q) {
-        const float4 f = __ldcg(reinterpret_cast<const float4 *>(p.part_mst + (row * p.parts + q) * 4));
-        const LpSum b = lp_rebase(LpSum{f.x, f.y, f.z}, to);
-        all.s += b.s; all.t += b.t;
-    }
+    // (every warp joins the sums by itself, a part a lane)
+    const float4 f = lane < p.parts ? __ldcg(reinterpret_cast<const float4 *>(p.part_mst + (row * p.parts + lane) * 4)) : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+    LpSum all{f.x, f.y, f.z};
+#pragma unroll
+    for (int s = 16; s >= 1; s >>= 1) m = fmaxf(s == 16 ? f.x : m, __shfl_xor_sync(0xffffffffu, s == 16 ? f.x : m, s));
+    all = lp_rebase(all, m > -INFINITY ? m : 0.0f);
+#pragma unroll
+    for (int s = 16; s >= 1; s >>= 1) { all.s += __shfl_xor_sync(0xffffffffu, all.s, s); all.t += __shfl_xor_sync(0xffffffffu, all.t, s); }
+    all.m = m;
     const int n = p.parts * p.k;
     for (int i = t; i < n; i += G) sh.list[i] = __ldcg(p.part_key + row * n + i);
     if (t < kLpMaxTop) sh.best[t] = 0ull;
     __syncthreads();
     lp_rank<G>(sh.list, n, p.k, sh.best, t);
     __syncthreads();
-    lp_finish<G, kIn32>(p, x, row, t, all, sh.best);
+    lp_finish<G, kIn32>(p, x, row, t, all, sh.best, lab0, x0);
 }
 
 }  // namespace xk

@@ -716,15 +716,16 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
             if (L.lp_parts_max > 1) {
                 // few rows: CTAs enough for two a unit, each with a chunk for every thread at least
                 const long long fill = 2ll * g.hw.sm_count / p.rows;
-                p.parts = (int)std::max(1ll, std::min(fill, std::min((long long)L.lp_parts_max, (long long)max_chunks / 512)));
+                p.parts = (int)std::max(1ll, std::min(fill, std::min((long long)L.lp_parts_max, (long long)max_chunks / 1024)));
             }
             p.part_chunks = (max_chunks + p.parts - 1) / p.parts;
             p.part_mst = (float *)(ws + g.split_off);
             p.part_key = (unsigned long long *)(ws + g.split_off + (size_t)2 * g.hw.sm_count * 16);
             p.arrived = (unsigned *)(ws + L.split_cnt_off);
-            if (L.C <= 2048) le = to.pdl(f32 ? xk::logprob_kernel<32, true> : xk::logprob_kernel<32, false>, (unsigned)((p.rows + 7) / 8), 256, 0, p);
-            else if (L.C <= kLpCtaEntries) le = to.pdl(f32 ? xk::logprob_kernel<128, true> : xk::logprob_kernel<128, false>, (unsigned)p.rows, 128, 0, p);
-            else le = to.pdl(f32 ? xk::logprob_kernel<512, true> : xk::logprob_kernel<512, false>, (unsigned)(p.rows * p.parts), 512, 0, p);
+            // fewer threads a row where the rows alone keep the SMs busy
+            if (L.C <= 2048) le = to.pdl(f32 ? xk::logprob_kernel<32, true> : xk::logprob_kernel<32, false>, (unsigned)((p.rows + 3) / 4), 128, 0, p);
+            else if (L.C <= kLpCtaEntries || p.rows >= 6ll * g.hw.sm_count) le = to.pdl(f32 ? xk::logprob_kernel<128, true> : xk::logprob_kernel<128, false>, (unsigned)p.rows, 128, 0, p);
+            else le = to.pdl(f32 ? xk::logprob_kernel<256, true> : xk::logprob_kernel<256, false>, (unsigned)(p.rows * p.parts), 256, 0, p);
             break;
         }
         case LK_GEMM2: {
