@@ -4,13 +4,14 @@
 //   norm       mu = mean(x), v = mean((x - mu)^2), y = (x - mu) / sqrt(v + eps) * gamma + beta
 //   to 8 bits  a = max |x|, q = round(127 x / a) (halves to even), scale = a / 127;  a = 0: q = 0
 //
-// Both are bound by HBM: the row is read once, kept in registers as fp32 and written once.  A group of G threads owns a row, each
-// thread V chunks of 8 consecutive channels (one 16-byte access of bf16, two of fp32); G and V are the smallest that hold the row, so
-// that short rows share a warp and no thread idles.  Mean and squared deviations are two reductions over the registers, not the
+// Both are bound by HBM: the row is read once, kept in registers in its own type and written once.  A group of G threads owns a row, each thread V
+// chunks of 8 channels (one 16-byte access of bf16, two of fp32).  A warp or less takes rows of up to 4096 bf16 channels (2048 of fp32): no barrier, the
+// loads of a whole row under way at once, and warps that are at different points of their rows keep memory busy (4096 bf16 channels:
+// 128 threads with two barriers a row 55.8 us for 16384 rows).  Mean and squared deviations are two reductions over the registers, not the
 // difference of two sums over memory, which would lose the digits of a variance that is small against the mean; the second one also sums
-// the deviations d, whose mean is the rounding of the first mean: (d - mean d) is exact to the last digits of d also for rows far from zero.
-// The reductions of a
-// group of several warps go through shared memory; gamma and beta come through L1, the row past it.
+// the deviations d, whose mean is the rounding of the first mean: (d - mean d) is exact to the last digits of d also for rows far from
+// zero.  The reductions of a group of several warps go through shared memory; gamma and beta come through L1, the row past it.
+// Rows that are not whole chunks (row_odd_kernel) are read and written channel by channel, a group's threads side by side.
 #pragma once
 
 #include "gemm_tc.cuh"
@@ -27,8 +28,17 @@ struct RowParams {
     long long rows;
     int C, pitch;
     float eps;
+    unsigned int *status;
+    int launch_id;
 };
 
+// Two fp32 values that one instruction works on.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair2(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void split2(f32x2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ uint4 ld_stream16(const void *p) {
     uint4 v;
     asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
@@ -104,162 +114,351 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t *red) {
     return row_reduce<G>(v, red, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
-// Threads of a CTA and rows it takes.  Short rows: 256 threads, and several rows per group so that enough bytes are under way.
+// Threads of a CTA and rows it takes: several rows per group of short rows, so that enough bytes are under way.
 template <int G, int V> struct RowShape {
-    static constexpr int threads = G <= 32 ? 256 : G;
-    static constexpr int per_group = G <= 32 ? (V >= 4 ? 1 : 4 / V) : 1;
+    static constexpr int threads = G <= 32 ? 128 : G;
+    static constexpr int per_group = G <= 32 && V < 4 ? 4 / V : 1;
     static constexpr int rows = threads / G * per_group;
 };
 
-// kVec: rows are whole chunks and 16-byte aligned; else a thread's channels are G apart and loaded one by one.
-template <int G, int V, bool kIn32, int kOut, bool kNorm, bool kVec>
+// Eight channels as four pairs.
+template <bool kIn32>
+__device__ __forceinline__ void row_pairs(const uint4 *u, f32x2 *e) {
+    if (kIn32) {
+        e[0] = pair2(__uint_as_float(u[0].x), __uint_as_float(u[0].y)); e[1] = pair2(__uint_as_float(u[0].z), __uint_as_float(u[0].w));
+        e[2] = pair2(__uint_as_float(u[1].x), __uint_as_float(u[1].y)); e[3] = pair2(__uint_as_float(u[1].z), __uint_as_float(u[1].w));
+    } else {
+        const uint32_t w[4] = {u[0].x, u[0].y, u[0].z, u[0].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = pair2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    }
+}
+__device__ __forceinline__ uint32_t pack2(f32x2 v) { float a, b; split2(v, a, b); return pack2(a, b); }
+
+// Eight normalised channels: two words of fp32 or one of bf16.
+template <bool kIn32, int kOut>
+__device__ __forceinline__ void row_norm8(const uint4 *u, uint4 *o, const f32x2 *ga, const f32x2 *be, f32x2 nmu, f32x2 rs, f32x2 noff) {
+    f32x2 e[4];
+    row_pairs<kIn32>(u, e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e[i] = fma2(fma2(add2(e[i], nmu), rs, noff), ga[i], be[i]);
+    if (kOut == RO_F32) {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split2(e[i], f[2 * i], f[2 * i + 1]);
+        o[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+        o[1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+    } else o[0] = make_uint4(pack2(e[0]), pack2(e[1]), pack2(e[2]), pack2(e[3]));
+}
+template <int kOut>
+__device__ __forceinline__ void row_store8(const RowParams &p, long long row, int c, const uint4 *o) {
+    if (kOut == RO_F32) {
+        uint4 *d = reinterpret_cast<uint4 *>(static_cast<float *>(p.y) + row * p.pitch + c);
+        d[0] = o[0]; d[1] = o[1];
+    } else *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.y) + row * p.pitch + c) = o[0];
+}
+// Largest magnitude so far, in the order of the bits (two of bf16 at a time).
+template <bool kWide>
+__device__ __forceinline__ void row_peak8(const uint4 *u, uint32_t &peak) {
+    if (kWide) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w) peak = max(max(max(peak, u[w].x & 0x7fffffffu), max(u[w].y & 0x7fffffffu, u[w].z & 0x7fffffffu)), u[w].w & 0x7fffffffu);
+    } else peak = __vmaxu2(__vmaxu2(__vmaxu2(peak, u[0].x & 0x7fff7fffu), __vmaxu2(u[0].y & 0x7fff7fffu, u[0].z & 0x7fff7fffu)), u[0].w & 0x7fff7fffu);
+}
+// Four values' low bytes in a word.
+__device__ __forceinline__ uint32_t row_bytes4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+template <bool kWide>
+__device__ __forceinline__ void row_quant8(const RowParams &p, long long row, int c, const uint4 *u, const RowScale &sc) {
+    f32x2 e[4];
+    row_pairs<kWide>(u, e);
+    uint32_t q[8];
+    if (!kWide && sc.lift != 1.0f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = mul2(e[i], pair2(sc.lift, sc.lift));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a, b;
+        if (kWide) {
+            split2(e[i], a, b);
+            q[2 * i] = row_quant<true>(a, sc); q[2 * i + 1] = row_quant<true>(b, sc);
+        } else {      // (row_quant<false> for two)
+            split2(mul2(e[i], pair2(sc.r, sc.r)), a, b);
+            a = __uint_as_float((__float_as_uint(a) + 16u) & 0xffffffe0u); b = __uint_as_float((__float_as_uint(b) + 16u) & 0xffffffe0u);
+            split2(add2(pair2(a, b), pair2(12582912.0f, 12582912.0f)), a, b);
+            q[2 * i] = __float_as_uint(a); q[2 * i + 1] = __float_as_uint(b);
+        }
+    }
+    *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + row * p.pitch + c) = make_uint2(row_bytes4(q[0], q[1], q[2], q[3]), row_bytes4(q[4], q[5], q[6], q[7]));
+}
+
+// Rows of whole chunks (channels a multiple of 8).
+template <int G, int V, bool kIn32, int kOut, bool kNorm>
 __global__ void __launch_bounds__(RowShape<G, V>::threads)
 row_kernel(const RowParams p) {
-    constexpr int R = RowShape<G, V>::per_group;
+    typedef RowShape<G, V> Shape;
+    constexpr int R = Shape::per_group, W = kIn32 ? 2 : 1;          // rows of a group; 16-byte words of a chunk
     __shared__ uint32_t red[4][32];
     pdl_launch_dependents();
     pdl_wait();
-    const int t = threadIdx.x % G, grp = threadIdx.x / G;
-    const long long row0 = (long long)blockIdx.x * RowShape<G, V>::rows + grp;
-    float x[R][V][8];
-    auto col = [&](int v, int i) { return kVec ? (v * G + t) * 8 + i : (v * 8 + i) * G + t; };
+    const int t = threadIdx.x % G;
+    const long long row0 = (long long)blockIdx.x * Shape::rows + threadIdx.x / G;
+    uint4 u[R][V][W];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const long long row = row0 + (long long)r * (RowShape<G, V>::threads / G);
-        const bool live = row < p.rows;
-        const long long base = row * p.C;
+        const long long row = row0 + (long long)r * (Shape::threads / G);
+        const char *base = static_cast<const char *>(p.x) + (row * p.C + t * 8) * (kIn32 ? 4 : 2);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (kVec) {
-                const bool in = live && col(v, 0) < p.C;
-                if (kIn32) {
-                    const float *q = static_cast<const float *>(p.x) + base + col(v, 0);
-                    const uint4 z = make_uint4(0, 0, 0, 0), a = in ? ld_stream16(q) : z, b = in ? ld_stream16(q + 4) : z;
-                    x[r][v][0] = __uint_as_float(a.x); x[r][v][1] = __uint_as_float(a.y); x[r][v][2] = __uint_as_float(a.z); x[r][v][3] = __uint_as_float(a.w);
-                    x[r][v][4] = __uint_as_float(b.x); x[r][v][5] = __uint_as_float(b.y); x[r][v][6] = __uint_as_float(b.z); x[r][v][7] = __uint_as_float(b.w);
-                } else {
-                    const f8 u = unpack8(in ? ld_stream16(static_cast<const __nv_bfloat16 *>(p.x) + base + col(v, 0)) : make_uint4(0, 0, 0, 0));
+        for (int v = 0; v < V; ++v)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[r][v][i] = u.v[i];
-                }
-            } else {
+            for (int w = 0; w < W; ++w)
+                u[r][v][w] = row < p.rows && (v * G + t) * 8 < p.C ? ld_stream16(base + v * G * 16 * W + w * 16) : make_uint4(0, 0, 0, 0);
+    }
+    f32x2 nmu[R], rs[R], noff[R];          // -mean, 1 / deviation, -(mean of the deviations) / deviation
+    if (kNorm) {
+        const float inv = 1.0f / (float)p.C;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int c = col(v, i);
-                    x[r][v][i] = !(live && c < p.C) ? 0.0f : kIn32 ? ld_scalar(static_cast<const float *>(p.x) + base + c)
-                                                                   : ld_scalar(static_cast<const __nv_bfloat16 *>(p.x) + base + c);
-                }
+        for (int r = 0; r < R; ++r) {
+            f32x2 s0 = 0ull, s1 = 0ull;                                // (zeros outside the row)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                f32x2 e[4];
+                row_pairs<kIn32>(u[r][v], e);
+                s0 = add2(s0, add2(e[0], e[1])); s1 = add2(s1, add2(e[2], e[3]));
+            }
+            float a, b;
+            split2(add2(s0, s1), a, b);
+            const float mu = __fdiv_rn(row_sum<G>(a + b, red[0]), (float)p.C);
+            nmu[r] = pair2(-mu, -mu);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            f32x2 s0 = 0ull, s1 = 0ull, q0 = 0ull, q1 = 0ull;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if ((v * G + t) * 8 >= p.C) continue;
+                f32x2 e[4];
+                row_pairs<kIn32>(u[r][v], e);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = add2(e[i], nmu[r]);
+                q0 = add2(q0, add2(e[0], e[1])); q1 = add2(q1, add2(e[2], e[3]));
+                s0 = fma2(e[0], e[0], s0); s1 = fma2(e[1], e[1], s1); s0 = fma2(e[2], e[2], s0); s1 = fma2(e[3], e[3], s1);
+            }
+            float a, b, c, d;
+            split2(add2(s0, s1), a, b); split2(add2(q0, q1), c, d);
+            const float2 f = row_sum2<G>(a + b, c + d, red[1], red[2]);
+            const float off = f.y * inv, rstd = rsqrtf(fmaxf(fmaf(f.x, inv, -off * off), 0.0f) + p.eps);
+            rs[r] = pair2(rstd, rstd); noff[r] = pair2(-off * rstd, -off * rstd);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const long long row = row0 + (long long)r * (Shape::threads / G);
+        if (kNorm) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int c = (v * G + t) * 8;
+                if (c >= p.C) continue;
+                // (a row that is rounded to 8 bits is rounded to bf16 first, as it would be between two kernels)
+                const uint4 *gp = reinterpret_cast<const uint4 *>(p.gamma + c), *bp = reinterpret_cast<const uint4 *>(p.beta + c);
+                const uint4 g[2] = {__ldg(gp), __ldg(gp + 1)}, b[2] = {__ldg(bp), __ldg(bp + 1)};
+                f32x2 ga[4], be[4];
+                row_pairs<true>(g, ga); row_pairs<true>(b, be);
+                uint4 o[2];
+                row_norm8<kIn32, kOut>(u[r][v], o, ga, be, nmu[r], rs[r], noff[r]);
+                if (kOut == RO_Q8) u[r][v][0] = o[0];
+                else if (row < p.rows) row_store8<kOut>(p, row, c, o);
             }
         }
+        if (kOut == RO_Q8) {
+            constexpr bool wide = kIn32 && !kNorm;
+            uint32_t peak = 0u;
+#pragma unroll
+            for (int v = 0; v < V; ++v) row_peak8<wide>(u[r][v], peak);
+            const RowScale sc = row_scale(row_max<G>(wide ? peak : max(peak << 16, peak & 0xffff0000u), red[3]));
+            if (row >= p.rows) continue;
+            if (t == 0) p.scale[row] = sc.scale;
+#pragma unroll
+            for (int v = 0; v < V; ++v)                                // (filled up to the pitch with zeros: u = 0 there)
+                if ((v * G + t) * 8 < p.pitch) row_quant8<wide>(p, row, (v * G + t) * 8, u[r][v], sc);
+        }
+    }
+}
+
+// Layer norm of many rows of whole chunks: groups of G threads that stay and walk over rows.  A thread keeps gamma and beta of its 8 V channels in
+// registers (read per row they are 64 bytes of L1 traffic for 16 of the row); the copy engine brings rows to shared memory, two per
+// group.  A row's slot is free for the next one as soon as the threads have it in registers, behind the first reduction, so loads are on their
+// way all the time.
+template <int G, int V, bool kIn32> struct StreamShape {
+    static constexpr int cta = G == 32 ? 128 : G;          // (larger groups are CTAs of their own: they meet at CTA barriers)
+    static constexpr int groups = G == 32 ? 4 : 1;
+    static constexpr int slots = 2;
+    static constexpr int resident = cta >= 512 ? 1 : 512 / cta;
+    // CTAs of an SM: as many as have some 64 KB of rows under way, 48 KB in small groups (measured, 268 MB in and out: 128 KB 52 us, 96 KB 47 to 50,
+    // 64 KB 45.5, 32 KB 59), at most 640 threads.
+    static int per_sm(int row_bytes) {
+        const int n = (G < 128 ? 48 : 64) * 1024 / (slots * groups * row_bytes), most = cta >= 640 ? 1 : 640 / cta;
+        return n < 1 ? 1 : n > most ? most : n;
+    }
+};
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+template <int G, int V, bool kIn32, int kOut>
+__global__ void __launch_bounds__(StreamShape<G, V, kIn32>::cta, StreamShape<G, V, kIn32>::resident)
+row_stream_kernel(const RowParams p) {
+    typedef StreamShape<G, V, kIn32> Shape;
+    constexpr int W = kIn32 ? 2 : 1, S = Shape::slots;
+    extern __shared__ __align__(128) uint8_t row_slots[];
+    __shared__ uint32_t red[4][32];
+    __shared__ __align__(8) unsigned long long full[Shape::groups][S];
+    pdl_launch_dependents();
+    const int t = threadIdx.x % G, grp = threadIdx.x / G;
+    const uint32_t bytes = (uint32_t)p.C * (kIn32 ? 4u : 2u), slots = smem_u32(row_slots) + (uint32_t)grp * S * bytes, bars = smem_u32(full[grp]);
+    if (t < S) mbar_init(bars + 8u * t, 1u);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    f32x2 ga[V][4], be[V][4];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int c = (v * G + t) * 8;
+        uint4 g[2], b[2];
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            g[w] = c < p.C ? __ldg(reinterpret_cast<const uint4 *>(p.gamma + c) + w) : make_uint4(0, 0, 0, 0);
+            b[w] = c < p.C ? __ldg(reinterpret_cast<const uint4 *>(p.beta + c) + w) : make_uint4(0, 0, 0, 0);
+        }
+        row_pairs<true>(g, ga[v]); row_pairs<true>(b, be[v]);
+    }
+    __syncthreads();
+    pdl_wait();
+    const long long step = (long long)gridDim.x * Shape::groups;
+    auto ask = [&](long long row, int s) {
+        if (t == 0 && row < p.rows) {
+            mbar_arrive_expect_tx(bars + 8u * s, bytes);
+            bulk_load(slots + (uint32_t)s * bytes, static_cast<const char *>(p.x) + row * (long long)bytes, bytes, bars + 8u * s);
+        }
+    };
+    const long long row0 = (long long)blockIdx.x * Shape::groups + grp;
+#pragma unroll
+    for (int s = 0; s < S; ++s) ask(row0 + s * step, s);
+    bool dead = false;                     // (a wait ran out: the rows that are left are walked over without waiting, so that every barrier is met)
+    int s = 0;
+    uint32_t ph = 0u;
+    const float inv = 1.0f / (float)p.C;
+#pragma unroll 1
+    for (long long row = row0; row < p.rows; row += step) {
+        if (!dead && !mbar_wait(bars + 8u * s, ph)) {
+            dead = true;
+            atomicCAS(p.status, 0u, kStatusTimeout | (3u << 8) | (((unsigned)p.launch_id & 0xfffu) << 12));
+        }
+        __syncwarp();
+        uint4 u[V][W];
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+                u[v][w] = (v * G + t) * 8 < p.C ? ld_shared16(slots + (uint32_t)s * bytes + (uint32_t)((v * G + t) * W + w) * 16u) : make_uint4(0, 0, 0, 0);
+        f32x2 s0 = 0ull, s1 = 0ull, q0 = 0ull, q1 = 0ull;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            f32x2 e[4];
+            row_pairs<kIn32>(u[v], e);
+            s0 = add2(s0, add2(e[0], e[1])); s1 = add2(s1, add2(e[2], e[3]));
+        }
+        float a, b, c, d;
+        split2(add2(s0, s1), a, b);
+        const float mu = __fdiv_rn(row_sum<G>(a + b, red[0]), (float)p.C);
+        ask(row + S * step, s);
+        if (++s == S) { s = 0; ph ^= 1u; }
+        const f32x2 nmu = pair2(-mu, -mu);
+        s0 = s1 = 0ull;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if ((v * G + t) * 8 >= p.C) continue;
+            f32x2 e[4];
+            row_pairs<kIn32>(u[v], e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = add2(e[i], nmu);
+            q0 = add2(q0, add2(e[0], e[1])); q1 = add2(q1, add2(e[2], e[3]));
+            s0 = fma2(e[0], e[0], s0); s1 = fma2(e[1], e[1], s1); s0 = fma2(e[2], e[2], s0); s1 = fma2(e[3], e[3], s1);
+        }
+        split2(add2(s0, s1), a, b); split2(add2(q0, q1), c, d);
+        const float2 f = row_sum2<G>(a + b, c + d, red[1], red[2]);
+        const float off = f.y * inv, rstd = rsqrtf(fmaxf(fmaf(f.x, inv, -off * off), 0.0f) + p.eps);
+        const f32x2 rs = pair2(rstd, rstd), noff = pair2(-off * rstd, -off * rstd);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c0 = (v * G + t) * 8;
+            if (c0 >= p.C) continue;
+            uint4 o[2];
+            row_norm8<kIn32, kOut>(u[v], o, ga[v], be[v], nmu, rs, noff);
+            row_store8<kOut>(p, row, c0, o);
+        }
+    }
+    if (dead) for (int i = 0; i < 64; ++i) __nanosleep(1000);      // (time for copies under way)
+}
+
+// Any rows: a thread's channels are G apart, one row a group.
+template <int G, int V, bool kIn32, int kOut, bool kNorm>
+__global__ void __launch_bounds__(G <= 32 ? 128 : G)
+row_odd_kernel(const RowParams p) {
+    constexpr int per_cta = G <= 32 ? 128 / G : 1;
+    __shared__ uint32_t red[4][32];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int t = threadIdx.x % G;
+    const long long row = (long long)blockIdx.x * per_cta + threadIdx.x / G;
+    const bool live = row < p.rows;
+    float x[8 * V];
+#pragma unroll
+    for (int i = 0; i < 8 * V; ++i) {
+        const int c = i * G + t;
+        x[i] = !(live && c < p.C) ? 0.0f : kIn32 ? ld_scalar(static_cast<const float *>(p.x) + row * p.C + c)
+                                                 : ld_scalar(static_cast<const __nv_bfloat16 *>(p.x) + row * p.C + c);
     }
     if (kNorm) {
         const float inv = 1.0f / (float)p.C;
-        float mu[R], rstd[R];
+        float s = 0.0f, e = 0.0f;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float s = 0.0f;
+        for (int i = 0; i < 8 * V; ++i) s += x[i];                      // (zeros outside the row)
+        const float mu = __fdiv_rn(row_sum<G>(s, red[0]), (float)p.C);
+        s = 0.0f;
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s += x[r][v][i];          // (zero outside the row)
-            mu[r] = __fdiv_rn(row_sum<G>(s, red[0]), (float)p.C);
+        for (int i = 0; i < 8 * V; ++i) {
+            x[i] = i * G + t < p.C ? x[i] - mu : 0.0f;
+            e += x[i];
+            s = fmaf(x[i], x[i], s);
         }
+        const float2 f = row_sum2<G>(s, e, red[1], red[2]);
+        const float off = f.y * inv, rstd = rsqrtf(fmaxf(fmaf(f.x, inv, -off * off), 0.0f) + p.eps);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float s = 0.0f, e = 0.0f;
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float d = col(v, i) < p.C ? x[r][v][i] - mu[r] : 0.0f;
-                    x[r][v][i] = d;
-                    e += d;
-                    s = fmaf(d, d, s);
-                }
-            const float2 f = row_sum2<G>(s, e, red[1], red[2]);
-            mu[r] = f.y * inv;                               // (of the deviations, from here on)
-            rstd[r] = rsqrtf(fmaxf(fmaf(f.x, inv, -mu[r] * mu[r]), 0.0f) + p.eps);
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            float ga[8], be[8];
-            if (kVec) {
-                const bool in = col(v, 0) < p.C;
-                const float4 z = make_float4(0, 0, 0, 0);
-                const float4 *gp = reinterpret_cast<const float4 *>(p.gamma + col(v, 0)), *bp = reinterpret_cast<const float4 *>(p.beta + col(v, 0));
-                const float4 g0 = in ? __ldg(gp) : z, g1 = in ? __ldg(gp + 1) : z, b0 = in ? __ldg(bp) : z, b1 = in ? __ldg(bp + 1) : z;
-                ga[0] = g0.x; ga[1] = g0.y; ga[2] = g0.z; ga[3] = g0.w; ga[4] = g1.x; ga[5] = g1.y; ga[6] = g1.z; ga[7] = g1.w;
-                be[0] = b0.x; be[1] = b0.y; be[2] = b0.z; be[3] = b0.w; be[4] = b1.x; be[5] = b1.y; be[6] = b1.z; be[7] = b1.w;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int c = col(v, i);
-                    ga[i] = c < p.C ? __ldg(p.gamma + c) : 0.0f; be[i] = c < p.C ? __ldg(p.beta + c) : 0.0f;
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float y = fmaf((x[r][v][i] - mu[r]) * rstd[r], ga[i], be[i]);
-                    // (a row that is rounded to 8 bits is rounded to bf16 first, as it would be between two kernels)
-                    if (kOut == RO_Q8) y = col(v, i) < p.C ? __bfloat162float(__float2bfloat16_rn(y)) : 0.0f;
-                    x[r][v][i] = y;
-                }
+        for (int i = 0; i < 8 * V; ++i) {
+            const int c = i * G + t;
+            if (c >= p.C) continue;
+            x[i] = fmaf(fmaf(x[i], rstd, -off * rstd), __ldg(p.gamma + c), __ldg(p.beta + c));
+            // (a row that is rounded to 8 bits is rounded to bf16 first, as it would be between two kernels)
+            if (kOut == RO_Q8) x[i] = __bfloat162float(__float2bfloat16_rn(x[i]));
         }
     }
+    RowScale sc;
+    if (kOut == RO_Q8) {
+        uint32_t m = 0;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const long long row = row0 + (long long)r * (RowShape<G, V>::threads / G);
-        const bool live = row < p.rows;
-        const long long base = row * p.pitch;
-        RowScale sc;
-        if (kOut == RO_Q8) {
-            uint32_t m = 0;
+        for (int i = 0; i < 8 * V; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+        sc = row_scale(row_max<G>(m, red[3]));
+        if (live && t == 0) p.scale[row] = sc.scale;
+    }
+    if (!live) return;
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[r][v][i]) & 0x7fffffffu);
-            sc = row_scale(row_max<G>(m, red[3]));
-            if (live && t == 0) p.scale[row] = sc.scale;
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (kOut == RO_Q8) {
-                uint32_t q[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) q[i] = row_quant<kIn32 && !kNorm>(x[r][v][i], sc);
-                // (the row is filled up to its pitch with zeros: x = 0 there)
-                if (kVec) {
-                    if (live && col(v, 0) < p.pitch)
-                        *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + base + col(v, 0)) =
-                            make_uint2(q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24, q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (live && col(v, i) < p.pitch) (static_cast<uint8_t *>(p.y) + base)[col(v, i)] = (uint8_t)q[i];
-                }
-            } else if (kVec) {
-                if (live && col(v, 0) < p.C) {
-                    if (kOut == RO_F32) {
-                        float4 *d = reinterpret_cast<float4 *>(static_cast<float *>(p.y) + base + col(v, 0));
-                        d[0] = make_float4(x[r][v][0], x[r][v][1], x[r][v][2], x[r][v][3]);
-                        d[1] = make_float4(x[r][v][4], x[r][v][5], x[r][v][6], x[r][v][7]);
-                    } else {
-                        f8 o;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) o.v[i] = x[r][v][i];
-                        *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(p.y) + base + col(v, 0)) = pack8(o);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (live && col(v, i) < p.C) {
-                        if (kOut == RO_F32) static_cast<float *>(p.y)[base + col(v, i)] = x[r][v][i];
-                        else static_cast<__nv_bfloat16 *>(p.y)[base + col(v, i)] = __float2bfloat16_rn(x[r][v][i]);
-                    }
-            }
+    for (int i = 0; i < 8 * V; ++i) {
+        const int c = i * G + t;
+        // (8-bit rows are filled up to the pitch with zeros: x = 0 there)
+        if (kOut == RO_Q8) { if (c < p.pitch) (static_cast<uint8_t *>(p.y) + row * p.pitch)[c] = (uint8_t)row_quant<kIn32 && !kNorm>(x[i], sc); }
+        else if (c < p.C) {
+            if (kOut == RO_F32) static_cast<float *>(p.y)[row * p.pitch + c] = x[i];
+            else static_cast<__nv_bfloat16 *>(p.y)[row * p.pitch + c] = __float2bfloat16_rn(x[i]);
         }
     }
 }

@@ -189,22 +189,54 @@ static xenos_status_t encode_bytes_map(const Graph &g, Runtime *rt, void *base, 
     return XENOS_OK;
 }
 
-// Layer norm / rounding of rows: the smallest group and number of chunks that hold `n` channels (rows_short), or the walk over memory.
+// Layer norm / rounding of rows: the smallest group and number of chunks that hold `n` channels, or the walk over memory.
 using RowKernel = void (*)(xk::RowParams);
 struct RowChoice { RowKernel kernel; int threads, rows; };
-template <int G, int V, bool kIn32, int kOut, bool kNorm, bool kVec>
-static RowChoice row_choice() { return {xk::row_kernel<G, V, kIn32, kOut, kNorm, kVec>, xk::RowShape<G, V>::threads, xk::RowShape<G, V>::rows}; }
+template <int G, int V, bool kIn32, int kOut, bool kNorm>
+static RowChoice row_choice() { return {xk::row_kernel<G, V, kIn32, kOut, kNorm>, xk::RowShape<G, V>::threads, xk::RowShape<G, V>::rows}; }
+template <int G, int V, bool kIn32, int kOut, bool kNorm>
+static RowChoice row_odd_choice() { return {xk::row_odd_kernel<G, V, kIn32, kOut, kNorm>, G <= 32 ? 128 : G, G <= 32 ? 128 / G : 1}; }
 template <bool kIn32, int kOut, bool kNorm>
 static RowChoice row_choice(int n, bool vec) {
     if (n > 16384) return {xk::row_long_kernel<kIn32, kOut, kNorm>, 512, 1};
     if (!vec)
-        return n <= 128 ? row_choice<8, 2, kIn32, kOut, kNorm, false>() : n <= 1024 ? row_choice<32, 4, kIn32, kOut, kNorm, false>()
-             : n <= 4096 ? row_choice<128, 4, kIn32, kOut, kNorm, false>() : row_choice<512, 4, kIn32, kOut, kNorm, false>();
-    return n <= 64 ? row_choice<8, 1, kIn32, kOut, kNorm, true>() : n <= 128 ? row_choice<8, 2, kIn32, kOut, kNorm, true>()
-         : n <= 256 ? row_choice<32, 1, kIn32, kOut, kNorm, true>() : n <= 512 ? row_choice<32, 2, kIn32, kOut, kNorm, true>()
-         : n <= 1024 ? row_choice<32, 4, kIn32, kOut, kNorm, true>() : n <= 2048 ? row_choice<128, 2, kIn32, kOut, kNorm, true>()
-         : n <= 4096 ? row_choice<128, 4, kIn32, kOut, kNorm, true>() : n <= 8192 ? row_choice<256, 4, kIn32, kOut, kNorm, true>()
-         : row_choice<512, 4, kIn32, kOut, kNorm, true>();
+        return n <= 128 ? row_odd_choice<8, 2, kIn32, kOut, kNorm>() : n <= 1024 ? row_odd_choice<32, 4, kIn32, kOut, kNorm>()
+             : n <= 4096 ? row_odd_choice<128, 4, kIn32, kOut, kNorm>() : row_odd_choice<512, 4, kIn32, kOut, kNorm>();
+    if (n <= 64) return row_choice<8, 1, kIn32, kOut, kNorm>();
+    if (n <= 128) return row_choice<8, 2, kIn32, kOut, kNorm>();
+    if (n <= 256) return row_choice<8, 4, kIn32, kOut, kNorm>();
+    if (n <= 512) return row_choice<16, 4, kIn32, kOut, kNorm>();
+    if (n <= 1024) return row_choice<32, 4, kIn32, kOut, kNorm>();
+    if (n <= 2048) return row_choice<32, 8, kIn32, kOut, kNorm>();
+    if (n <= 4096) return kIn32 ? row_choice<128, 4, kIn32, kOut, kNorm>() : row_choice<64, 8, kIn32, kOut, kNorm>();
+    if (n <= 8192) return row_choice<128, 8, kIn32, kOut, kNorm>();
+    return row_choice<256, 8, kIn32, kOut, kNorm>();
+}
+// Layer norm of many rows of 257 to 16384 channels (8192 of fp32): CTAs that stay.  kernel null: too few rows to fill them several times, or rows of
+// another length.  (8-bit results take a third reduction a row, which more and smaller groups hide better: 8192 rows of 4096 35 us, here 38.)
+struct StreamChoice { RowKernel kernel; int threads, grid, smem; };
+template <int G, int V, bool kIn32, int kOut>
+static StreamChoice stream_choice(const Launch &L, long long rows, int sms) {
+    typedef xk::StreamShape<G, V, kIn32> Shape;
+    const int bytes = L.C * (kIn32 ? 4 : 2), grid = Shape::per_sm(bytes) * sms;
+    if (rows < 4ll * grid * Shape::groups) return {nullptr, 0, 0, 0};
+    return {xk::row_stream_kernel<G, V, kIn32, kOut>, Shape::cta, grid, Shape::slots * Shape::groups * bytes};
+}
+template <int kOut>
+static StreamChoice stream_choice(const Launch &L, long long rows, int sms) {
+    const int n = L.C;
+    if (!L.row_norm || n % 8 || n <= 256 || n > (L.row_in_f32 ? 8192 : 16384)) return {nullptr, 0, 0, 0};
+    if (L.row_in_f32)
+        return n <= 512 ? stream_choice<32, 2, true, kOut>(L, rows, sms) : n <= 1024 ? stream_choice<64, 2, true, kOut>(L, rows, sms)
+             : n <= 2048 ? stream_choice<128, 2, true, kOut>(L, rows, sms) : n <= 4096 ? stream_choice<256, 2, true, kOut>(L, rows, sms)
+             : stream_choice<512, 2, true, kOut>(L, rows, sms);
+    return n <= 512 ? stream_choice<32, 2, false, kOut>(L, rows, sms) : n <= 1024 ? stream_choice<32, 4, false, kOut>(L, rows, sms)
+         : n <= 2048 ? stream_choice<64, 4, false, kOut>(L, rows, sms) : n <= 4096 ? stream_choice<128, 4, false, kOut>(L, rows, sms)
+         : n <= 8192 ? stream_choice<256, 4, false, kOut>(L, rows, sms) : stream_choice<512, 4, false, kOut>(L, rows, sms);
+}
+static StreamChoice stream_choice(const Launch &L, long long rows, int sms) {
+    if (L.row_out == xk::RO_Q8) return {nullptr, 0, 0, 0};
+    return L.row_out == xk::RO_F32 ? stream_choice<xk::RO_F32>(L, rows, sms) : stream_choice<xk::RO_BF16>(L, rows, sms);
 }
 template <bool kIn32>
 static RowChoice row_choice(const Launch &L) {
@@ -360,9 +392,10 @@ private:
     cudaError_t issue(const void *kernel, dim3 grid, dim3 block, int smem, int cluster, bool programmatic, void **argv) const {
         if (mode == READY) {
             // the first mention of a kernel loads its code.  The opt-in limit is a per-function, per-device setting shared by
-            // every graph in the process: always the device's maximum, so that binding one graph never lowers it for another.
+            // every graph in the process: always the most that the device and the kernel's static arrays allow, so that binding one graph never lowers it for another.
             cudaFuncAttributes at;
-            return smem > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, optin) : cudaFuncGetAttributes(&at, kernel);
+            const cudaError_t e = cudaFuncGetAttributes(&at, kernel);
+            return e != cudaSuccess || smem <= 48 * 1024 ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, optin - (int)at.sharedSizeBytes);
         }
         if (mode == POINT) {
             cudaKernelNodeParams p = {};
@@ -670,6 +703,12 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
             p.y = L.row_out == xk::RO_Q8 ? scratch : ptr(L.out);
             p.scale = (float *)(scratch + L.q_scale_off);
             p.rows = (long long)N * L.rows_per_image; p.C = L.C; p.pitch = L.row_out == xk::RO_Q8 ? L.q_pitch : L.C; p.eps = L.eps;
+            p.status = status; p.launch_id = (int)li;
+            const StreamChoice stay = stream_choice(L, p.rows, sms);
+            if (stay.kernel) {
+                le = to.pdl(stay.kernel, stay.grid, stay.threads, stay.smem, p);
+                break;
+            }
             const RowChoice k = L.row_in_f32 ? row_choice<true>(L) : row_choice<false>(L);
             le = to.pdl(k.kernel, (unsigned)((p.rows + k.rows - 1) / k.rows), k.threads, 0, p);
             break;

@@ -283,6 +283,52 @@ def test_norm_keeps_what_is_not_finite_in_its_row():
     assert np.isnan(got[hit]).all() and np.array_equal(got[~hit], clean[~hit])
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,c", [(20001, 264), (9000, 512), (7500, 1000), (7301, 1024), (5003, 1032), (3700, 2048), (2500, 4000), (2400, 4096), (1300, 5000),
+                                    (1200, 8192), (700, 16384), (601, 12000)])
+def test_norm_of_many_rows(rows, c):
+    """Enough rows for the CTAs that stay and walk over them; the last round of rows does not fill them."""
+    for kind, out in (("bf16", "bf16"), ("f32", "f32")):
+        build, batch, x, gamma, beta = norm_case(rows, c, kind, out, 5)
+        got, = Rows(build, batch).run([to_device(x, kind)], batch)
+        check_norm(got, rounded(x, kind), gamma, beta, out)
+
+
+@pytest.mark.gpu
+def test_rows_whose_offsets_pass_32_bits():
+    """More than 2^31 elements: the last rows of a layer norm and of a row of scores."""
+    import torch
+    c, rows = 32768, 65535 + 4
+    h = 3
+    batch = -(-rows // h)
+    rows = batch * h
+    x = torch.empty((rows, c), dtype=torch.bfloat16, device="cuda")
+    x[:-2] = 0
+    tail = rng_of("far").standard_normal((2, c))
+    x[-2:] = torch.from_numpy(tail).to(torch.bfloat16).cuda()
+    gamma = np.ones(c, np.float32)
+
+    def norm(g):
+        t = g.add_input(xb.DTYPE_BF16, xb.LAYOUT_NHWC, c, h, 1)
+        return [(g.add_op(xb.OP_LAYERNORM, [t], weight=gamma), c, "bf16")]
+
+    def answers(g):
+        t = g.add_input(xb.DTYPE_BF16, xb.LAYOUT_NHWC, c, h, 1)
+        lp, ent, ids, tops = g.add_logprob(t, None, 3)
+        return [(ent, 1, "f32"), (ids, 3, "i32"), (tops, 3, "f32")]
+    xt = rounded(tail, "bf16")
+    r = Rows(answers, batch, (h, 1))
+    got = r.run([x], batch)
+    check_lp([a[-2:] for a in got], xt, None, 3)
+    r = Rows(norm, batch, (h, 1))
+    y = torch.empty((rows + 1, c), dtype=torch.bfloat16, device="cuda")
+    y[-1] = -77
+    r.g.run(batch, [x.data_ptr()], [y.data_ptr()], r.stream)
+    r.g.status(r.stream)
+    check_norm(y[-3:-1].double().cpu().numpy(), xt, gamma, np.zeros(c), "bf16")
+    assert bool((y[-1] == -77).all()) and not bool(y[0].any())
+
+
 # ---- the product in 8-bit integers -------------------------------------------------------------------------------------------
 def q8_case(rows, c, n, kind, out, act, bias, seed):
     rng = rng_of(rows, c, n, kind, out, act, seed)
