@@ -280,7 +280,8 @@ inline int out_dim(int in, int k, int stride, int pad) {
 }
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
-constexpr int kQ8SmallRows = 16;         // rows up to which q8_small_kernel takes an 8-bit product
+constexpr int kQ8SmallRows = 16;         // rows up to which q8_small_kernel takes an 8-bit product,
+constexpr int kQ8SmallSmem = 160 * 1024; // ... where the rows in 8 bits fit
 constexpr int kLpCtaEntries = 8192;      // entries above which a row of scores may have CTAs of 256 threads, and several of them
 
 // Channel tile of an 8-bit product in tiles of one CTA: modelled cycles.  A block of 128 deep takes the slower of the tensor pipe (2 cycles a

@@ -245,7 +245,7 @@ static bool try_match(const LinkCtx &cx, int a, Allowed allowed, Chain &out, boo
         // itself (q8_small_kernel): there the link would only replace its one launch.  (A layer norm whose result others read too is not linked.)
         const int b = cx.sole(a);
         if (b < 0 || !allowed(b) || g.nodes[b].kind != NK_QMATMUL) return false;
-        if (by_model && (long long)g.max_batch * g.tensors[A.out].rows() <= kQ8SmallRows) return false;
+        if (by_model && (long long)g.max_batch * g.tensors[A.out].rows() <= kQ8SmallRows && A.cin <= kQ8SmallSmem / kQ8SmallRows - 192) return false;
         out.kind = CK_NORM_QMATMUL;
         out.nodes = {a, b};
         out.pattern = "LayerNorm -> 8-bit product (row-wise producer and consumer)";
@@ -1639,7 +1639,8 @@ struct Lower {
         L.w2_off = put_f32(n.w); L.b_off = put_f32(n.b);
         L.flops = 2.0 * node_macs(n);
         L.bytes = tbytes(n.out) + node_param_bytes(n);
-        if (!norm && rows <= kQ8SmallRows) {
+        L.smem_bytes = (int)std::min<long long>(rows * (L.q_pitch + 64), 1 << 30);
+        if (!norm && rows <= kQ8SmallRows && L.smem_bytes <= std::min(kQ8SmallSmem, g.hw.smem_bytes_per_cta - 12 * 1024)) {
             L.kind = LK_Q8_SMALL;
             L.in0 = src;
             L.row_in_f32 = elem_dtype(g, src) == XENOS_DTYPE_F32;

@@ -15,8 +15,8 @@
 //
 // q8_small_kernel (up to 16 rows): a pass over the weights, bound by their bytes.  A CTA owns 16 channels, its 8 warps share the
 // depth; mma.sync takes the channels as its 16 rows and the activation's rows as its 8 columns (tcgen05 has no shape that reads
-// weights from registers).  The weights are asked for before the predecessor is waited for; each CTA then finds the rows' scales by itself and
-// rounds the values that it needs: no second launch.
+// weights from registers).  The weights (512 bytes of depth a warp and channel) are asked for before the predecessor is waited for; each CTA then
+// finds the rows' scales and rounds the rows to shared memory by itself: no second launch.
 #pragma once
 
 #include "conv_tc.cuh"
@@ -296,44 +296,39 @@ __device__ __forceinline__ void mma_s8(int *c, const uint32_t *a, const uint32_t
     asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
-// 16 consecutive values of a row from k on (zeros behind the row).
+// Eight consecutive values of a row from k on (zeros behind the row).
 template <bool kIn32>
 __device__ __forceinline__ void q8_values(const Q8SmallParams &g, int m, int k, float *v) {
-    if (m >= g.M || k >= g.K) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = 0.0f;
-    } else if (g.vec && k + 16 <= g.K) {
+    if (g.vec && k + 8 <= g.K) {
         if (kIn32) {
             const float4 *q = reinterpret_cast<const float4 *>(static_cast<const float *>(g.x) + (size_t)m * g.K + k);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { const float4 f = q[i]; v[4 * i] = f.x; v[4 * i + 1] = f.y; v[4 * i + 2] = f.z; v[4 * i + 3] = f.w; }
+            const float4 a = q[0], b = q[1];
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
         } else {
-            const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(g.x) + (size_t)m * g.K + k);
+            const f8 f = unpack8(*reinterpret_cast<const uint4 *>(static_cast<const __nv_bfloat16 *>(g.x) + (size_t)m * g.K + k));
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const f8 f = unpack8(q[i]);
-#pragma unroll
-                for (int c = 0; c < 8; ++c) v[8 * i + c] = f.v[c];
-            }
+            for (int i = 0; i < 8; ++i) v[i] = f.v[i];
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
+        for (int i = 0; i < 8; ++i)
             v[i] = k + i >= g.K ? 0.0f : kIn32 ? static_cast<const float *>(g.x)[(size_t)m * g.K + k + i]
                                                : __bfloat162float(static_cast<const __nv_bfloat16 *>(g.x)[(size_t)m * g.K + k + i]);
     }
 }
 
-// kN: rows of the activation in eights.
+// kN: rows of the activation in eights.  Shared memory: the rows rounded to 8 bits, pitch + 64 bytes apart (the lanes of a fragment's load then meet
+// all banks).
 template <int kN, bool kIn32>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 2)
 q8_small_kernel(const Q8SmallParams g) {
-    constexpr int U = 4;
+    constexpr int U = 8;
+    extern __shared__ __align__(16) uint8_t q8_rows[];
     __shared__ uint32_t peak[8 * kN];
     __shared__ int sums[8][8 * kN][17];
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane >> 2, q = lane & 3;
-    const int n0 = blockIdx.x * 16;
+    const int n0 = blockIdx.x * 16, ld = g.pitch + 64;
     // a step is 64 bytes of depth: the lane's 16 bytes of two channels are the operand of two products, in an order of the depth that both
     // operands share
     const uint8_t *wa = g.w + (size_t)min(n0 + grp, g.N - 1) * g.pitch + q * 16, *wb = g.w + (size_t)min(n0 + 8 + grp, g.N - 1) * g.pitch + q * 16;
@@ -343,35 +338,49 @@ q8_small_kernel(const Q8SmallParams g) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int s = s0 + 8 * u;
-            a[u] = b[u] = make_uint4(0, 0, 0, 0);
             if (s < steps) { a[u] = ld_stream16(wa + (size_t)s * 64); b[u] = ld_stream16(wb + (size_t)s * 64); }
         }
     };
     fetch(warp);
     if (threadIdx.x < 8 * kN) peak[threadIdx.x] = 0u;
-    pdl_wait();
     __syncthreads();
-    // ---- largest magnitude of every row: each warp its share of the depth
-    for (int m = 0; m < g.M; ++m) {
+    pdl_wait();
+    // ---- the rows' largest magnitudes, then their values: 256, 128, 64 or 32 threads a row (whole warps)
+    const int lg = g.M <= 1 ? 8 : g.M <= 2 ? 7 : g.M <= 4 ? 6 : 5, tr = threadIdx.x & ((1 << lg) - 1);
+    for (int m = threadIdx.x >> lg; m < g.M; m += 256 >> lg) {
         uint32_t mx = 0;
-        for (int k = threadIdx.x * 16; k < g.K; k += 256 * 16) {
-            float v[16];
+#pragma unroll 4
+        for (int k = tr * 8; k < g.K; k += 8 << lg) {
+            float v[8];
             q8_values<kIn32>(g, m, k, v);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) mx = max(mx, __float_as_uint(v[i]) & 0x7fffffffu);
+            for (int i = 0; i < 8; ++i) mx = max(mx, __float_as_uint(v[i]) & 0x7fffffffu);
         }
         mx = __reduce_max_sync(0xffffffffu, mx);
-        if (lane == 0 && mx) atomicMax(&peak[m], mx);
+        if (lane == 0) atomicMax(&peak[m], mx);
     }
     __syncthreads();
-    RowScale sc[kN];
+    for (int m = threadIdx.x >> lg; m < g.M; m += 256 >> lg) {
+        const RowScale sc = row_scale(peak[m]);
+#pragma unroll 2
+        for (int k = tr * 8; k < g.pitch; k += 8 << lg) {
+            float v[8];
+            q8_values<kIn32>(g, m, k, v);
+            uint32_t x[8];
 #pragma unroll
-    for (int n = 0; n < kN; ++n) sc[n] = row_scale(peak[n * 8 + grp]);
+            for (int i = 0; i < 8; ++i) x[i] = row_quant<kIn32>(v[i], sc);
+            *reinterpret_cast<uint2 *>(q8_rows + (size_t)m * ld + k) = make_uint2(row_bytes4(x[0], x[1], x[2], x[3]), row_bytes4(x[4], x[5], x[6], x[7]));
+        }
+    }
+    __syncthreads();
     int acc[kN][4];
+    uint32_t at[kN];                       // (columns behind the last row repeat it; nobody reads their sums)
 #pragma unroll
-    for (int n = 0; n < kN; ++n)
+    for (int n = 0; n < kN; ++n) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[n][i] = 0;
+        at[n] = smem_u32(q8_rows) + (uint32_t)(min(n * 8 + grp, g.M - 1) * ld + q * 16);
+    }
 #pragma unroll 1
     for (int s0 = warp; s0 < steps; s0 += 8 * U) {
         if (s0 != warp) fetch(s0);
@@ -381,12 +390,8 @@ q8_small_kernel(const Q8SmallParams g) {
             if (s >= steps) break;
 #pragma unroll
             for (int n = 0; n < kN; ++n) {
-                float v[16];
-                q8_values<kIn32>(g, n * 8 + grp, s * 64 + q * 16, v);
-                uint32_t x[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    x[i] = row_quant<kIn32>(v[4 * i], sc[n]) | row_quant<kIn32>(v[4 * i + 1], sc[n]) << 8 | row_quant<kIn32>(v[4 * i + 2], sc[n]) << 16 | row_quant<kIn32>(v[4 * i + 3], sc[n]) << 24;
+                const uint4 xv = ld_shared16(at[n] + (uint32_t)s * 64u);
+                const uint32_t x[4] = {xv.x, xv.y, xv.z, xv.w};
                 const uint32_t a0[4] = {a[u].x, b[u].x, a[u].y, b[u].y}, a1[4] = {a[u].z, b[u].z, a[u].w, b[u].w};
                 mma_s8(acc[n], a0, x);
                 mma_s8(acc[n], a1, x + 2);

@@ -395,7 +395,7 @@ private:
             // every graph in the process: always the most that the device and the kernel's static arrays allow, so that binding one graph never lowers it for another.
             cudaFuncAttributes at;
             const cudaError_t e = cudaFuncGetAttributes(&at, kernel);
-            return e != cudaSuccess || smem <= 48 * 1024 ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, optin - (int)at.sharedSizeBytes);
+            return e != cudaSuccess || smem == 0 ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, optin - (int)at.sharedSizeBytes);
         }
         if (mode == POINT) {
             cudaKernelNodeParams p = {};
@@ -457,6 +457,7 @@ static xenos_status_t attach(Graph &g, void *ws, void *stream_v) {
     int max_gemm_smem = 0, max_chain_smem = 0;
     for (const Launch &L : g.launches) {
         if (L.kind == LK_GEMM2) { any_gemm = true; max_gemm_smem = std::max(max_gemm_smem, L.smem_bytes); }
+        if (L.kind == LK_Q8_SMALL) max_gemm_smem = std::max(max_gemm_smem, L.smem_bytes + 10 * 1024);
         if (L.kind == LK_Q8) { any_gemm = true; max_gemm_smem = std::max(max_gemm_smem, L.smem_bytes); }
         if (L.kind == LK_GEMM) { any_gemm = true; max_gemm_smem = std::max(max_gemm_smem, L.smem_bytes); }
         if (L.kind == LK_F32_CONV_CONV_POOL) {
@@ -738,9 +739,9 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
             p.x = ptr(L.in0); p.w = ws + L.w_off; p.ws = (const float *)(ws + L.w2_off); p.bias = (const float *)(ws + L.b_off); p.y = ptr(L.out);
             p.M = N * L.rows_per_image; p.N = L.K; p.K = L.C; p.pitch = L.q_pitch; p.act = L.act; p.out_f32 = L.out_dtype == XENOS_DTYPE_F32;
             p.vec = L.C % (L.row_in_f32 ? 4 : 8) == 0;
-            const int grid = (L.K + 15) / 16;
-            if (L.row_in_f32) le = to.pdl(p.M <= 8 ? xk::q8_small_kernel<1, true> : xk::q8_small_kernel<2, true>, grid, 256, 0, p);
-            else le = to.pdl(p.M <= 8 ? xk::q8_small_kernel<1, false> : xk::q8_small_kernel<2, false>, grid, 256, 0, p);
+            const int grid = (L.K + 15) / 16, smem = p.M * (L.q_pitch + 64);
+            if (L.row_in_f32) le = to.pdl(p.M <= 8 ? xk::q8_small_kernel<1, true> : xk::q8_small_kernel<2, true>, grid, 256, smem, p);
+            else le = to.pdl(p.M <= 8 ? xk::q8_small_kernel<1, false> : xk::q8_small_kernel<2, false>, grid, 256, smem, p);
             break;
         }
         case LK_LOGPROB: {
