@@ -280,8 +280,9 @@ inline int out_dim(int in, int k, int stride, int pad) {
 }
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
-constexpr int kQ8SmallRows = 16;         // rows up to which q8_small_kernel takes an 8-bit product,
-constexpr int kQ8SmallSmem = 160 * 1024; // ... where the rows in 8 bits fit
+// Rows, and values of all rows, up to which an 8-bit product goes through q8_small_kernel.
+constexpr int kQ8SmallRows = 16, kQ8SelfValues = 16384;
+inline bool q8_self(long long rows, int c) { return rows <= kQ8SmallRows && rows * ((c + 127) / 128 * 128) <= kQ8SelfValues; }
 constexpr int kLpCtaEntries = 8192;      // entries above which a row of scores may have CTAs of 256 threads, and several of them
 
 // Channel tile of an 8-bit product in tiles of one CTA: modelled cycles.  A block of 128 deep takes the slower of the tensor pipe (2 cycles a
@@ -291,9 +292,10 @@ inline double q8_cycles(long long rows, int N, int kblocks, int units, int tile_
     const double block = tile_n * 2.0 > (16384 + tile_n * 128) / 75.0 ? tile_n * 2.0 : (16384 + tile_n * 128) / 75.0;
     return (double)(long long)((tiles + units - 1) / units) * (kblocks * block + 300.0 + 6.0 * tile_n) + 1000.0;
 }
-// Shared memory of a launch of q8_tc_kernel: 1024 to align, ring, a 4 KB box and 256 bytes of parameters per epilogue warp, barriers.
-constexpr int kQ8FixedSmem = 1024 + 8 * (4096 + 256) + 256;
-inline int q8_stage_bytes(int tile_n, bool pair) { return 16384 + (pair ? 128 : tile_n) * 128; }
+// Shared memory of a launch of q8_tc_kernel: 1024 to align, ring, a 4 KB box and 1 KB of parameters per epilogue warp, barriers.
+constexpr int kQ8FixedSmem = 1024 + 8 * (4096 + 1024) + 256;
+inline int q8_per_stage(int tile_n, bool pair) { return !pair && tile_n <= 64 ? 2 : 1; }      // blocks of 128 deep: a thread's looks at the barriers take 200 cycles each
+inline int q8_stage_bytes(int tile_n, bool pair) { return (16384 + (pair ? 128 : tile_n) * 128) * q8_per_stage(tile_n, pair); }
 inline int q8_stages(const xenos_hw_info_t &hw, int tile_n, bool pair) {
     const int cap = hw.smem_bytes_per_cta < 227 * 1024 ? hw.smem_bytes_per_cta : 227 * 1024, n = (cap - kQ8FixedSmem) / q8_stage_bytes(tile_n, pair);
     return n > 8 ? 8 : n;

@@ -241,11 +241,11 @@ static bool try_match(const LinkCtx &cx, int a, Allowed allowed, Chain &out, boo
     }
     // ---- bf16 tensor-core chains -----------------------------------------------------------
     if (A.kind == NK_NORM) {
-        // the normalised row leaves as the 8-bit values and the scale that the product reads.  A product of few rows rounds its rows by
+        // the normalised row leaves as the 8-bit values and the scale that the product reads.  A product of few values rounds its rows by
         // itself (q8_small_kernel): there the link would only replace its one launch.  (A layer norm whose result others read too is not linked.)
         const int b = cx.sole(a);
         if (b < 0 || !allowed(b) || g.nodes[b].kind != NK_QMATMUL) return false;
-        if (by_model && (long long)g.max_batch * g.tensors[A.out].rows() <= kQ8SmallRows && A.cin <= kQ8SmallSmem / kQ8SmallRows - 192) return false;
+        if (by_model && q8_self((long long)g.max_batch * g.tensors[A.out].rows(), A.cin)) return false;
         out.kind = CK_NORM_QMATMUL;
         out.nodes = {a, b};
         out.pattern = "LayerNorm -> 8-bit product (row-wise producer and consumer)";
@@ -1598,7 +1598,7 @@ struct Lower {
         if (norm) { L.w_off = put_f32(norm->w); L.b_off = put_f32(norm->b); L.eps = norm->eps; }
         if (out == 2) {
             L.q_pitch = round_up(x.c, 128);
-            const long long rows = (long long)g.max_batch * L.rows_per_image;
+            const long long rows = ((long long)g.max_batch * L.rows_per_image + 127) / 128 * 128;
             L.q_scale_off = align_up((size_t)rows * L.q_pitch, 256);
             L.scratch_bytes = L.q_scale_off + align_up((size_t)rows * 4, 256);
         }
@@ -1639,8 +1639,7 @@ struct Lower {
         L.w2_off = put_f32(n.w); L.b_off = put_f32(n.b);
         L.flops = 2.0 * node_macs(n);
         L.bytes = tbytes(n.out) + node_param_bytes(n);
-        L.smem_bytes = (int)std::min<long long>(rows * (L.q_pitch + 64), 1 << 30);
-        if (!norm && rows <= kQ8SmallRows && L.smem_bytes <= std::min(kQ8SmallSmem, g.hw.smem_bytes_per_cta - 12 * 1024)) {
+        if (!norm && q8_self(rows, n.cin)) {
             L.kind = LK_Q8_SMALL;
             L.in0 = src;
             L.row_in_f32 = elem_dtype(g, src) == XENOS_DTYPE_F32;

@@ -15,8 +15,10 @@
 //
 // q8_small_kernel (up to 16 rows): a pass over the weights, bound by their bytes.  A CTA owns 16 channels, its 8 warps share the
 // depth; mma.sync takes the channels as its 16 rows and the activation's rows as its 8 columns (tcgen05 has no shape that reads
-// weights from registers).  The weights (512 bytes of depth a warp and channel) are asked for before the predecessor is waited for; each CTA then
-// finds the rows' scales and rounds the rows to shared memory by itself: no second launch.
+// weights from registers).  The weights (512 bytes of depth a warp and channel, and while those are used the next) are asked for before the predecessor is waited
+// for.  Each CTA stays for several sets of channels where there are many; it finds the rows' scales and
+// rounds the rows to shared memory by itself: no second launch, but work that every CTA repeats, so the rule is 16384 values in all (4096 x 4096: 4
+// rows 7.1 us here and 10.4 there; 16 rows 19 and 10.4).
 #pragma once
 
 #include "conv_tc.cuh"
@@ -33,6 +35,8 @@ struct Q8Params {
     unsigned int *status;
     int M, N, kblocks;             // rows, channels, blocks of 128 deep
     int tile_n, m_tiles, n_tiles, stages, stage_bytes, tmem_cols;
+    int per_stage;                 // blocks of a stage: 2 where a tile is narrow
+    uint32_t a_bytes;              // a box of the activation (its rows x 128)
     int act, out_f32, vec;         // vec: rows of the result are whole 16-byte pieces
     int off_stage, off_par, off_bar;
     uint32_t idesc;
@@ -60,15 +64,38 @@ __device__ __forceinline__ void q8_commit(uint32_t bar) {
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((unsigned short)3) : "memory");
     else umma_commit(bar);
 }
+// The products of a stage (four of 32 deep per block of 128, `two` blocks or one), their commit to the barrier that frees it, and the
+// state of the next stage's barrier: asked for first, looked at last (see umma_block).  Descriptors' lower halves in 16-byte units; a_next, b_next:
+// distance of the second block's operands.
+#define XENOS_Q8_STAGE(GROUP, COMMIT)                                                                                                          \
+    asm volatile(                                                                                                                              \
+        "{\n\t.reg .pred p, q, w;\n\t.reg .b64 da, db;\n\t.reg .b32 x, y;\n\t"                                                                  \
+        "mbarrier.test_wait.parity.shared::cta.b64 q, [%11], %12;\n\t"                                                                         \
+        "setp.ne.b32 p, %8, 0;\n\tsetp.ne.b32 w, %9, 0;\n\t"                                                                                   \
+        "mov.b64 da, {%3, %2};\n\tmov.b64 db, {%4, %2};\n\ttcgen05.mma." GROUP ".kind::i8 [%1], da, db, %7, p;\n\tsetp.eq.u32 p, 0, 0;\n\t"   \
+        "add.u32 x, %3, 2;\n\tadd.u32 y, %4, 2;\n\tmov.b64 da, {x, %2};\n\tmov.b64 db, {y, %2};\n\ttcgen05.mma." GROUP ".kind::i8 [%1], da, db, %7, p;\n\t" \
+        "add.u32 x, %3, 4;\n\tadd.u32 y, %4, 4;\n\tmov.b64 da, {x, %2};\n\tmov.b64 db, {y, %2};\n\ttcgen05.mma." GROUP ".kind::i8 [%1], da, db, %7, p;\n\t" \
+        "add.u32 x, %3, 6;\n\tadd.u32 y, %4, 6;\n\tmov.b64 da, {x, %2};\n\tmov.b64 db, {y, %2};\n\ttcgen05.mma." GROUP ".kind::i8 [%1], da, db, %7, p;\n\t" \
+        "add.u32 x, %3, %5;\n\tadd.u32 y, %4, %6;\n\tmov.b64 da, {x, %2};\n\tmov.b64 db, {y, %2};\n\t@w tcgen05.mma." GROUP ".kind::i8 [%1], da, db, %7, p;\n\t" \
+        "add.u32 x, x, 2;\n\tadd.u32 y, y, 2;\n\tmov.b64 da, {x, %2};\n\tmov.b64 db, {y, %2};\n\t@w tcgen05.mma." GROUP ".kind::i8 [%1], da, db, %7, p;\n\t" \
+        "add.u32 x, x, 2;\n\tadd.u32 y, y, 2;\n\tmov.b64 da, {x, %2};\n\tmov.b64 db, {y, %2};\n\t@w tcgen05.mma." GROUP ".kind::i8 [%1], da, db, %7, p;\n\t" \
+        "add.u32 x, x, 2;\n\tadd.u32 y, y, 2;\n\tmov.b64 da, {x, %2};\n\tmov.b64 db, {y, %2};\n\t@w tcgen05.mma." GROUP ".kind::i8 [%1], da, db, %7, p;\n\t" \
+        COMMIT "selp.u32 %0, 1, 0, q;\n\t}"                                                                                                    \
+        : "=r"(ready)                                                                                                                          \
+        : "r"(d), "r"(hi), "r"(a), "r"(b), "r"(a_next), "r"(b_next), "r"(idesc), "r"(acc), "r"(two), "r"(freed), "r"(next), "r"(next_ph), "h"((unsigned short)3) \
+        : "memory")
 template <int kPair>
-__device__ __forceinline__ void q8_mma(uint32_t d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t acc) {
+__device__ __forceinline__ uint32_t q8_stage(uint32_t d, uint32_t a, uint32_t b, uint32_t a_next, uint32_t b_next, uint32_t idesc, uint32_t acc, uint32_t two,
+                                             uint32_t freed, uint32_t next, uint32_t next_ph) {
+    constexpr uint32_t hi = 64u | (1u << 14) | (2u << 29);      // 128-byte swizzle, 1024-byte groups
+    uint32_t ready;
     if (kPair == 2)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
-                     ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(acc) : "memory");
+        XENOS_Q8_STAGE("cta_group::2", "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%10], %13;\n\t");
     else
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
-                     ::"r"(d), "l"(da), "l"(db), "r"(idesc), "r"(acc) : "memory");
+        XENOS_Q8_STAGE("cta_group::1", "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%10];\n\t");
+    return ready;
 }
+#undef XENOS_Q8_STAGE
 // One arrival at the barrier with this offset in the tile's first CTA.
 template <int kPair>
 __device__ __forceinline__ void q8_arrive_first(uint32_t bar) {
@@ -136,9 +163,10 @@ q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CU
         // ---- operands: 128 rows of the activation, tile_n channels of the weights (a pair: 128 each) ----
         if (elect_one()) {
             const bool act = warp == 0;
-            const int boxes = act ? 1 : kPair == 1 && g.tile_n == 256 ? 2 : 1;
-            const uint32_t bytes = act ? 16384u * kPair : (uint32_t)g.tile_n * 128u;       // what arrives at the tile's first CTA
-            const uint32_t off = act ? 0u : 16384u;
+            const int boxes = !act && kPair == 1 && g.tile_n == 256 ? 2 : 1, per = in_reg(g.per_stage);
+            const uint32_t box = act ? g.a_bytes : (uint32_t)min(g.tile_n, 128) * 128u;
+            const uint32_t bytes = box * boxes * kPair, step_k = act ? 16384u : (uint32_t)g.tile_n * 128u;      // what a block delivers; where the next one goes
+            const uint32_t off = act ? 0u : 16384u * per;
             const CUtensorMap *tm = act ? &tmA : &tmB;
             const int kblocks = in_reg(g.kblocks), stages = in_reg(g.stages);
             if (act) pdl_wait();
@@ -149,12 +177,14 @@ q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CU
                 const Q8Tile t = q8_tile(g, ti);
                 const int row = act ? (t.mt * kPair + rank) * 128 : t.nt * g.tile_n + rank * 128;
 #pragma unroll 1
-                for (int kb = 0; kb < kblocks; ++kb) {
+                for (int kb = 0; kb < kblocks; kb += per) {
                     if (n >= stages && !mbar_wait(empty_bar(s), ph)) { ok = false; break; }
                     const uint32_t dst = sbase + (uint32_t)s * g.stage_bytes + off;
-                    if (rank == 0) mbar_arrive_expect_tx(full_bar(s), bytes);
+                    const bool two = per == 2 && kb + 1 < kblocks;
+                    if (rank == 0) mbar_arrive_expect_tx(full_bar(s), two ? 2 * bytes : bytes);
                     q8_load<kPair>(dst, tm, kb * 128, row, full_bar(s));
                     if (boxes == 2) q8_load<kPair>(dst + 16384u, tm, kb * 128, row + 128, full_bar(s));
+                    if (two) q8_load<kPair>(dst + step_k, tm, kb * 128 + 128, row, full_bar(s));
                     ++n;
                     if (++s == stages) { s = 0; ph ^= 1u; }
                 }
@@ -170,10 +200,11 @@ q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CU
     } else if (warp == 1 && rank == 0) {
         // ---- products ----
         if (elect_one()) {
-            const int kblocks = in_reg(g.kblocks), stages = in_reg(g.stages);
-            const uint32_t idesc = in_reg(g.idesc);
+            const int kblocks = in_reg(g.kblocks), stages = in_reg(g.stages), per = in_reg(g.per_stage);
+            const uint32_t idesc = in_reg(g.idesc), stage16 = in_reg((uint32_t)g.stage_bytes >> 4), first16 = 0x10000u | (sbase >> 4);
+            const uint32_t b_off = 1024u * per, b_next = in_reg((uint32_t)g.tile_n * 8u);
             int s = 0, i = 0;
-            uint32_t ph = 0u;
+            uint32_t ph = 0u, ready = 0u, a16 = first16;
 #pragma unroll 1
             for (int ti = first; ti < total && ok; ti += step, ++i) {
                 const int b = i & 1;
@@ -181,13 +212,14 @@ q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CU
                 tc_fence_after();
                 const uint32_t d = tmem_base + (uint32_t)(b * g.tile_n);
 #pragma unroll 1
-                for (int kb = 0; kb < kblocks; ++kb) {
-                    if (!mbar_wait(full_bar(s), ph)) { ok = false; break; }
-                    const uint64_t da = umma_desc_sw128(sbase + (uint32_t)s * g.stage_bytes), db = umma_desc_sw128(sbase + (uint32_t)s * g.stage_bytes + 16384u);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) q8_mma<kPair>(d, da + 2 * k, db + 2 * k, idesc, kb + k ? 1u : 0u);
-                    q8_commit<kPair>(empty_bar(s));
-                    if (++s == stages) { s = 0; ph ^= 1u; }
+                for (int kb = 0; kb < kblocks; kb += per) {
+                    if (!ready && !mbar_wait(full_bar(s), ph)) { ok = false; break; }
+                    const uint32_t freed = empty_bar(s), now = a16;
+                    const bool wrap = s + 1 == stages;
+                    s = wrap ? 0 : s + 1;
+                    a16 = wrap ? first16 : a16 + stage16;
+                    ph ^= wrap ? 1u : 0u;
+                    ready = q8_stage<kPair>(d, now, now + b_off, 1024u, b_next, idesc, kb, per == 2 && kb + 1 < kblocks, freed, full_bar(s), ph);
                 }
                 if (ok) q8_commit<kPair>(accf_bar(b));
             }
@@ -199,7 +231,7 @@ q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CU
         const int e = warp - 4, quarter = warp & 3, half = e >> 2;
         const uint32_t t_warp = tmem_base + ((uint32_t)(quarter * 32) << 16);
         uint8_t *box = sm + g.off_stage + e * 4096;
-        float *par = reinterpret_cast<float *>(sm + g.off_par + e * 256);
+        float *pars = reinterpret_cast<float *>(sm + g.off_par + e * 1024);
         const int chunks = g.tile_n / 32;
         int i = 0;
 #pragma unroll 1
@@ -207,24 +239,37 @@ q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CU
             const Q8Tile t = q8_tile(g, ti);
             const int b = i & 1, m0 = (t.mt * kPair + rank) * 128 + quarter * 32;
             const float sx = m0 + lane < g.M ? g.xs[m0 + lane] : 0.0f;
+            // scales and biases of the warp's chunks, on their way while the tile is multiplied
+            float wv[4], bv[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int x = t.nt * g.tile_n + (half + 2 * c) * 32 + lane;
+                const bool in = half + 2 * c < chunks && x < g.N;
+                wv[c] = in ? __ldg(g.ws + x) : 0.0f; bv[c] = in ? __ldg(g.bias + x) : 0.0f;
+            }
+            __syncwarp();                                        // (those of the tile before have been read)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) { pars[c * 64 + lane] = wv[c]; pars[c * 64 + 32 + lane] = bv[c]; }
             if (!mbar_wait(accf_bar(b), (i >> 1) & 1)) { ok = false; break; }
             tc_fence_after();
 #pragma unroll 1
             for (int j = half; j < chunks; j += 2) {
                 const int x0 = t.nt * g.tile_n + j * 32, x = x0 + lane;
-                __syncwarp();                                    // (the box and the parameters of the chunk before have been read)
-                par[lane] = x < g.N ? __ldg(g.ws + x) : 0.0f;
-                par[32 + lane] = x < g.N ? __ldg(g.bias + x) : 0.0f;
+                const float *par = pars + (j >> 1) * 64;
                 float v[32];
                 tmem_ld32(t_warp + b * g.tile_n + j * 32, v);
-                __syncwarp();
+                __syncwarp();                                    // (the box of the chunk before has been read)
 #pragma unroll
                 for (int c = 0; c < 32; c += 4) {
                     const float4 w = *reinterpret_cast<const float4 *>(par + c), bb = *reinterpret_cast<const float4 *>(par + 32 + c);
-                    v[c] = q8_act(fmaf((float)__float_as_int(v[c]), sx * w.x, bb.x), g.act);
-                    v[c + 1] = q8_act(fmaf((float)__float_as_int(v[c + 1]), sx * w.y, bb.y), g.act);
-                    v[c + 2] = q8_act(fmaf((float)__float_as_int(v[c + 2]), sx * w.z, bb.z), g.act);
-                    v[c + 3] = q8_act(fmaf((float)__float_as_int(v[c + 3]), sx * w.w, bb.w), g.act);
+                    v[c] = fmaf((float)__float_as_int(v[c]), sx * w.x, bb.x);
+                    v[c + 1] = fmaf((float)__float_as_int(v[c + 1]), sx * w.y, bb.y);
+                    v[c + 2] = fmaf((float)__float_as_int(v[c + 2]), sx * w.z, bb.z);
+                    v[c + 3] = fmaf((float)__float_as_int(v[c + 3]), sx * w.w, bb.w);
+                }
+                if (g.act) {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) v[c] = q8_act(v[c], g.act);
                 }
                 if (g.out_f32) {
 #pragma unroll
@@ -328,20 +373,19 @@ q8_small_kernel(const Q8SmallParams g) {
     __shared__ int sums[8][8 * kN][17];
     pdl_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = lane >> 2, q = lane & 3;
-    const int n0 = blockIdx.x * 16, ld = g.pitch + 64;
+    const int ld = g.pitch + 64, sets = (g.N + 15) / 16;
     // a step is 64 bytes of depth: the lane's 16 bytes of two channels are the operand of two products, in an order of the depth that both
     // operands share
-    const uint8_t *wa = g.w + (size_t)min(n0 + grp, g.N - 1) * g.pitch + q * 16, *wb = g.w + (size_t)min(n0 + 8 + grp, g.N - 1) * g.pitch + q * 16;
     const int steps = g.pitch / 64;
     uint4 a[U], b[U];
-    auto fetch = [&](int s0) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int s = s0 + 8 * u;
-            if (s < steps) { a[u] = ld_stream16(wa + (size_t)s * 64); b[u] = ld_stream16(wb + (size_t)s * 64); }
-        }
+    // step s of a set of channels (none behind the last)
+    auto fetch = [&](int u, int set, int s) {
+        if (s >= steps || set >= sets) return;
+        const uint8_t *w = g.w + (size_t)s * 64 + q * 16;
+        a[u] = ld_stream16(w + (size_t)min(set * 16 + grp, g.N - 1) * g.pitch); b[u] = ld_stream16(w + (size_t)min(set * 16 + 8 + grp, g.N - 1) * g.pitch);
     };
-    fetch(warp);
+#pragma unroll
+    for (int u = 0; u < U; ++u) fetch(u, blockIdx.x, warp + 8 * u);
     if (threadIdx.x < 8 * kN) peak[threadIdx.x] = 0u;
     __syncthreads();
     pdl_wait();
@@ -373,48 +417,55 @@ q8_small_kernel(const Q8SmallParams g) {
         }
     }
     __syncthreads();
-    int acc[kN][4];
     uint32_t at[kN];                       // (columns behind the last row repeat it; nobody reads their sums)
 #pragma unroll
-    for (int n = 0; n < kN; ++n) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[n][i] = 0;
-        at[n] = smem_u32(q8_rows) + (uint32_t)(min(n * 8 + grp, g.M - 1) * ld + q * 16);
-    }
+    for (int n = 0; n < kN; ++n) at[n] = smem_u32(q8_rows) + (uint32_t)(min(n * 8 + grp, g.M - 1) * ld + q * 16);
 #pragma unroll 1
-    for (int s0 = warp; s0 < steps; s0 += 8 * U) {
-        if (s0 != warp) fetch(s0);
+    for (int set = blockIdx.x; set < sets; set += gridDim.x) {
+        int acc[kN][4];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int s = s0 + 8 * u;
-            if (s >= steps) break;
+        for (int n = 0; n < kN; ++n)
 #pragma unroll
-            for (int n = 0; n < kN; ++n) {
-                const uint4 xv = ld_shared16(at[n] + (uint32_t)s * 64u);
-                const uint32_t x[4] = {xv.x, xv.y, xv.z, xv.w};
-                const uint32_t a0[4] = {a[u].x, b[u].x, a[u].y, b[u].y}, a1[4] = {a[u].z, b[u].z, a[u].w, b[u].w};
-                mma_s8(acc[n], a0, x);
-                mma_s8(acc[n], a1, x + 2);
+            for (int i = 0; i < 4; ++i) acc[n][i] = 0;
+#pragma unroll 1
+        for (int s0 = warp; s0 < steps; s0 += 8 * U) {
+            const bool last = s0 + 8 * U >= steps;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int s = s0 + 8 * u;
+                if (s < steps) {
+#pragma unroll
+                    for (int n = 0; n < kN; ++n) {
+                        const uint4 xv = ld_shared16(at[n] + (uint32_t)s * 64u);
+                        const uint32_t x[4] = {xv.x, xv.y, xv.z, xv.w};
+                        const uint32_t a0[4] = {a[u].x, b[u].x, a[u].y, b[u].y}, a1[4] = {a[u].z, b[u].z, a[u].w, b[u].w};
+                        mma_s8(acc[n], a0, x);
+                        mma_s8(acc[n], a1, x + 2);
+                    }
+                }
+                if (last) fetch(u, set + gridDim.x, warp + 8 * u);
+                else fetch(u, set, s + 8 * U);
             }
         }
-    }
-    // ---- the warps' sums
+        // ---- the warps' sums
 #pragma unroll
-    for (int n = 0; n < kN; ++n) {
-        sums[warp][n * 8 + 2 * q][grp] = acc[n][0]; sums[warp][n * 8 + 2 * q + 1][grp] = acc[n][1];
-        sums[warp][n * 8 + 2 * q][grp + 8] = acc[n][2]; sums[warp][n * 8 + 2 * q + 1][grp + 8] = acc[n][3];
-    }
-    __syncthreads();
-    if (threadIdx.x < 128 * kN) {
-        const int m = threadIdx.x >> 4, c = threadIdx.x & 15, n = n0 + c;
-        if (m < g.M && n < g.N) {
-            int s = 0;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) s += sums[w][m][c];
-            const float r = q8_act(fmaf((float)s, row_scale(peak[m]).scale * __ldg(g.ws + n), __ldg(g.bias + n)), g.act);
-            if (g.out_f32) static_cast<float *>(g.y)[(size_t)m * g.N + n] = r;
-            else static_cast<__nv_bfloat16 *>(g.y)[(size_t)m * g.N + n] = __float2bfloat16_rn(r);
+        for (int n = 0; n < kN; ++n) {
+            sums[warp][n * 8 + 2 * q][grp] = acc[n][0]; sums[warp][n * 8 + 2 * q + 1][grp] = acc[n][1];
+            sums[warp][n * 8 + 2 * q][grp + 8] = acc[n][2]; sums[warp][n * 8 + 2 * q + 1][grp + 8] = acc[n][3];
         }
+        __syncthreads();
+        if (threadIdx.x < 128 * kN) {
+            const int m = threadIdx.x >> 4, c = threadIdx.x & 15, n = set * 16 + c;
+            if (m < g.M && n < g.N) {
+                int s = 0;
+#pragma unroll
+                for (int w = 0; w < 8; ++w) s += sums[w][m][c];
+                const float r = q8_act(fmaf((float)s, row_scale(peak[m]).scale * __ldg(g.ws + n), __ldg(g.bias + n)), g.act);
+                if (g.out_f32) static_cast<float *>(g.y)[(size_t)m * g.N + n] = r;
+                else static_cast<__nv_bfloat16 *>(g.y)[(size_t)m * g.N + n] = __float2bfloat16_rn(r);
+            }
+        }
+        __syncthreads();
     }
 }
 

@@ -400,7 +400,7 @@ row_stream_kernel(const RowParams p) {
     if (dead) for (int i = 0; i < 64; ++i) __nanosleep(1000);      // (time for copies under way)
 }
 
-// Any rows: a thread's channels are G apart, one row a group.
+// Any rows, one a group: a thread's channels are G apart, or four together where they leave as 8-bit values (a word of them).
 template <int G, int V, bool kIn32, int kOut, bool kNorm>
 __global__ void __launch_bounds__(G <= 32 ? 128 : G)
 row_odd_kernel(const RowParams p) {
@@ -411,13 +411,12 @@ row_odd_kernel(const RowParams p) {
     const int t = threadIdx.x % G;
     const long long row = (long long)blockIdx.x * per_cta + threadIdx.x / G;
     const bool live = row < p.rows;
+    auto col = [&](int i) { return kOut == RO_Q8 ? ((i >> 2) * G + t) * 4 + (i & 3) : i * G + t; };
     float x[8 * V];
 #pragma unroll
-    for (int i = 0; i < 8 * V; ++i) {
-        const int c = i * G + t;
-        x[i] = !(live && c < p.C) ? 0.0f : kIn32 ? ld_scalar(static_cast<const float *>(p.x) + row * p.C + c)
-                                                 : ld_scalar(static_cast<const __nv_bfloat16 *>(p.x) + row * p.C + c);
-    }
+    for (int i = 0; i < 8 * V; ++i)
+        x[i] = !(live && col(i) < p.C) ? 0.0f : kIn32 ? ld_scalar(static_cast<const float *>(p.x) + row * p.C + col(i))
+                                                      : ld_scalar(static_cast<const __nv_bfloat16 *>(p.x) + row * p.C + col(i));
     if (kNorm) {
         const float inv = 1.0f / (float)p.C;
         float s = 0.0f, e = 0.0f;
@@ -427,7 +426,7 @@ row_odd_kernel(const RowParams p) {
         s = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8 * V; ++i) {
-            x[i] = i * G + t < p.C ? x[i] - mu : 0.0f;
+            x[i] = col(i) < p.C ? x[i] - mu : 0.0f;
             e += x[i];
             s = fmaf(x[i], x[i], s);
         }
@@ -435,32 +434,127 @@ row_odd_kernel(const RowParams p) {
         const float off = f.y * inv, rstd = rsqrtf(fmaxf(fmaf(f.x, inv, -off * off), 0.0f) + p.eps);
 #pragma unroll
         for (int i = 0; i < 8 * V; ++i) {
-            const int c = i * G + t;
+            const int c = col(i);
             if (c >= p.C) continue;
             x[i] = fmaf(fmaf(x[i], rstd, -off * rstd), __ldg(p.gamma + c), __ldg(p.beta + c));
             // (a row that is rounded to 8 bits is rounded to bf16 first, as it would be between two kernels)
             if (kOut == RO_Q8) x[i] = __bfloat162float(__float2bfloat16_rn(x[i]));
         }
     }
-    RowScale sc;
     if (kOut == RO_Q8) {
         uint32_t m = 0;
 #pragma unroll
         for (int i = 0; i < 8 * V; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
-        sc = row_scale(row_max<G>(m, red[3]));
-        if (live && t == 0) p.scale[row] = sc.scale;
+        const RowScale sc = row_scale(row_max<G>(m, red[3]));
+        if (!live) return;
+        if (t == 0) p.scale[row] = sc.scale;
+#pragma unroll
+        for (int i = 0; i < 8 * V; i += 4) {
+            uint32_t q[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) q[k] = row_quant<kIn32 && !kNorm>(x[i + k], sc);
+            // (rows are filled up to the pitch with zeros: x = 0 there)
+            if (col(i) < p.pitch) *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(p.y) + row * p.pitch + col(i)) = row_bytes4(q[0], q[1], q[2], q[3]);
+        }
+        return;
     }
     if (!live) return;
 #pragma unroll
     for (int i = 0; i < 8 * V; ++i) {
+        const int c = col(i);
+        if (c >= p.C) continue;
+        if (kOut == RO_F32) static_cast<float *>(p.y)[row * p.pitch + c] = x[i];
+        else static_cast<__nv_bfloat16 *>(p.y)[row * p.pitch + c] = __float2bfloat16_rn(x[i]);
+    }
+}
+
+// Layer norm of many rows of any length, as row_stream_kernel: a thread's channels are G apart, so that gamma and beta stay in registers whatever the
+// rows' alignment; the copy engine brings the 16-byte pieces that a row meets, its neighbours' ends with them, but nothing behind the tensor (the
+// last row's end is read from where it is).
+template <int G, int V, bool kIn32, int kOut>
+__global__ void __launch_bounds__(G, 512 / G)
+row_stream_odd_kernel(const RowParams p) {
+    constexpr int S = 2, ES = kIn32 ? 4 : 2, N = 8 * V;
+    extern __shared__ __align__(128) uint8_t row_slots[];
+    __shared__ uint32_t red[3][32];
+    __shared__ __align__(8) unsigned long long full[S];
+    pdl_launch_dependents();
+    const int t = threadIdx.x;
+    const uint32_t slot = ((uint32_t)p.C * ES + 15u & ~15u) + 16u, slots = smem_u32(row_slots), bars = smem_u32(full);
+    if (t < S) mbar_init(bars + 8u * t, 1u);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    float ga[N], be[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
         const int c = i * G + t;
-        // (8-bit rows are filled up to the pitch with zeros: x = 0 there)
-        if (kOut == RO_Q8) { if (c < p.pitch) (static_cast<uint8_t *>(p.y) + row * p.pitch)[c] = (uint8_t)row_quant<kIn32 && !kNorm>(x[i], sc); }
-        else if (c < p.C) {
-            if (kOut == RO_F32) static_cast<float *>(p.y)[row * p.pitch + c] = x[i];
-            else static_cast<__nv_bfloat16 *>(p.y)[row * p.pitch + c] = __float2bfloat16_rn(x[i]);
+        ga[i] = c < p.C ? __ldg(p.gamma + c) : 0.0f; be[i] = c < p.C ? __ldg(p.beta + c) : 0.0f;
+    }
+    __syncthreads();
+    pdl_wait();
+    auto ask = [&](long long row, int s) {
+        if (t != 0 || row >= p.rows) return;
+        const unsigned long long from = row * (unsigned long long)(p.C * ES), to = from + (unsigned)(p.C * ES);
+        const unsigned long long a = from & ~15ull, b = row + 1 < p.rows ? (to + 15) & ~15ull : to & ~15ull;
+        const uint32_t bytes = b > a ? (uint32_t)(b - a) : 0u;
+        mbar_arrive_expect_tx(bars + 8u * s, bytes);
+        if (bytes) bulk_load(slots + (uint32_t)s * slot, static_cast<const char *>(p.x) + a, bytes, bars + 8u * s);
+    };
+#pragma unroll
+    for (int s = 0; s < S; ++s) ask(blockIdx.x + (long long)s * gridDim.x, s);
+    bool dead = false;                     // (a wait ran out: the rows that are left are walked over without waiting, so that every barrier is met)
+    int s = 0;
+    uint32_t ph = 0u;
+    const float inv = 1.0f / (float)p.C;
+#pragma unroll 1
+    for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        if (!dead && !mbar_wait(bars + 8u * s, ph)) {
+            dead = true;
+            atomicCAS(p.status, 0u, kStatusTimeout | (3u << 8) | (((unsigned)p.launch_id & 0xfffu) << 12));
+        }
+        const unsigned long long from = row * (unsigned long long)(p.C * ES);
+        const uint32_t lead = (uint32_t)(from & 15ull);
+        // channels that came by copy
+        const int came = row + 1 < p.rows ? p.C : (int)(((from + (unsigned)(p.C * ES)) & ~15ull) > from ? (((from + (unsigned)(p.C * ES)) & ~15ull) - from) / ES : 0);
+        const uint8_t *at = row_slots + (size_t)s * slot + lead;
+        float x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = i * G + t;
+            if (kIn32) x[i] = c < came ? reinterpret_cast<const float *>(at)[c] : 0.0f;
+            else x[i] = c < came ? __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(at)[c]) : 0.0f;
+        }
+        if (came < p.C) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int c = i * G + t;
+                if (c >= came && c < p.C) x[i] = kIn32 ? ld_scalar(static_cast<const float *>(p.x) + row * p.C + c) : ld_scalar(static_cast<const __nv_bfloat16 *>(p.x) + row * p.C + c);
+            }
+        }
+        float a = 0.0f, e = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) a += x[i];
+        const float mu = __fdiv_rn(row_sum<G>(a, red[0]), (float)p.C);
+        ask(row + (long long)S * gridDim.x, s);
+        if (++s == S) { s = 0; ph ^= 1u; }
+        a = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            x[i] = i * G + t < p.C ? x[i] - mu : 0.0f;
+            e += x[i];
+            a = fmaf(x[i], x[i], a);
+        }
+        const float2 f = row_sum2<G>(a, e, red[1], red[2]);
+        const float off = f.y * inv, rstd = rsqrtf(fmaxf(fmaf(f.x, inv, -off * off), 0.0f) + p.eps);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = i * G + t;
+            if (c >= p.C) continue;
+            const float y = fmaf(fmaf(x[i], rstd, -off * rstd), ga[i], be[i]);
+            if (kOut == RO_F32) static_cast<float *>(p.y)[row * p.pitch + c] = y;
+            else static_cast<__nv_bfloat16 *>(p.y)[row * p.pitch + c] = __float2bfloat16_rn(y);
         }
     }
+    if (dead) for (int i = 0; i < 64; ++i) __nanosleep(1000);      // (time for copies under way)
 }
 
 // Rows that no group holds in registers (more than 16384 channels): a CTA walks over its row once per pass, from L2 after the first.

@@ -222,9 +222,20 @@ static StreamChoice stream_choice(const Launch &L, long long rows, int sms) {
     if (rows < 4ll * grid * Shape::groups) return {nullptr, 0, 0, 0};
     return {xk::row_stream_kernel<G, V, kIn32, kOut>, Shape::cta, grid, Shape::slots * Shape::groups * bytes};
 }
+// ... of rows that are not whole chunks: bf16 only (16384 rows of 4095: 107 us one row a CTA, 72 here; of fp32 50 either way).
+template <int G, int kOut>
+static StreamChoice stream_odd_choice(const Launch &L, long long rows, int sms) {
+    const int grid = 512 / G * sms;
+    if (rows < 4ll * grid) return {nullptr, 0, 0, 0};
+    return {xk::row_stream_odd_kernel<G, 4, false, kOut>, G, grid, 2 * (int)(align_up((size_t)L.C * 2, 16) + 16)};
+}
 template <int kOut>
 static StreamChoice stream_choice(const Launch &L, long long rows, int sms) {
     const int n = L.C;
+    if (L.row_norm && n % 8 && n > 256 && n <= 16384 && !L.row_in_f32)
+        return n <= 1024 ? stream_odd_choice<32, kOut>(L, rows, sms) : n <= 2048 ? stream_odd_choice<64, kOut>(L, rows, sms)
+             : n <= 4096 ? stream_odd_choice<128, kOut>(L, rows, sms) : n <= 8192 ? stream_odd_choice<256, kOut>(L, rows, sms)
+             : stream_odd_choice<512, kOut>(L, rows, sms);
     if (!L.row_norm || n % 8 || n <= 256 || n > (L.row_in_f32 ? 8192 : 16384)) return {nullptr, 0, 0, 0};
     if (L.row_in_f32)
         return n <= 512 ? stream_choice<32, 2, true, kOut>(L, rows, sms) : n <= 1024 ? stream_choice<64, 2, true, kOut>(L, rows, sms)
@@ -457,7 +468,6 @@ static xenos_status_t attach(Graph &g, void *ws, void *stream_v) {
     int max_gemm_smem = 0, max_chain_smem = 0;
     for (const Launch &L : g.launches) {
         if (L.kind == LK_GEMM2) { any_gemm = true; max_gemm_smem = std::max(max_gemm_smem, L.smem_bytes); }
-        if (L.kind == LK_Q8_SMALL) max_gemm_smem = std::max(max_gemm_smem, L.smem_bytes + 10 * 1024);
         if (L.kind == LK_Q8) { any_gemm = true; max_gemm_smem = std::max(max_gemm_smem, L.smem_bytes); }
         if (L.kind == LK_GEMM) { any_gemm = true; max_gemm_smem = std::max(max_gemm_smem, L.smem_bytes); }
         if (L.kind == LK_F32_CONV_CONV_POOL) {
@@ -502,9 +512,11 @@ static xenos_status_t attach(Graph &g, void *ws, void *stream_v) {
             }
             if (L.kind == LK_Q8) {
                 // activation rows in the split scratch; weights in boxes of 32, 64 and 128 channels, for the tile widths that runs choose
-                const long long rows = (long long)g.max_batch * L.rows_per_image;
-                uint8_t *w = static_cast<uint8_t *>(ws) + L.w_off;
-                xenos_status_t st = encode_bytes_map(g, rt, static_cast<uint8_t *>(ws) + g.split_off, L.q_pitch, rows, 128, &rt->tmaps[i]);
+                // (the scratch holds whole boxes of rows: a box that reaches behind the tensor takes twice the time)
+                const long long rows = ((long long)g.max_batch * L.rows_per_image + 127) / 128 * 128;
+                uint8_t *w = static_cast<uint8_t *>(ws) + L.w_off, *q = static_cast<uint8_t *>(ws) + g.split_off;
+                xenos_status_t st = encode_bytes_map(g, rt, q, L.q_pitch, rows, 128, &rt->tmaps[i]);
+                if (st == XENOS_OK) st = encode_bytes_map(g, rt, q, L.q_pitch, rows, 64, &rt->hmaps[i]);
                 if (st == XENOS_OK) st = encode_bytes_map(g, rt, w, L.q_pitch, L.K, 32, &rt->conv[i].a0);
                 if (st == XENOS_OK) st = encode_bytes_map(g, rt, w, L.q_pitch, L.K, 64, &rt->conv[i].a1);
                 if (st == XENOS_OK) st = encode_bytes_map(g, rt, w, L.q_pitch, L.K, 128, &rt->conv[i].o);
@@ -724,14 +736,19 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
             p.xs = (const float *)(ws + g.split_off + L.q_scale_off); p.ws = (const float *)(ws + L.w2_off); p.bias = (const float *)(ws + L.b_off);
             p.y = ptr(L.out); p.status = status; p.act = L.act; p.out_f32 = L.out_dtype == XENOS_DTYPE_F32; p.vec = L.K % (p.out_f32 ? 4 : 8) == 0;
             p.stages = q8_stages(g.hw, p.tile_n, pair); p.stage_bytes = q8_stage_bytes(p.tile_n, pair); p.tmem_cols = std::max(32, 2 * p.tile_n);
-            p.off_stage = p.stages * p.stage_bytes; p.off_par = p.off_stage + 8 * 4096; p.off_bar = p.off_par + 8 * 256;
+            p.off_stage = p.stages * p.stage_bytes; p.off_par = p.off_stage + 8 * 4096; p.off_bar = p.off_par + 8 * 1024;
             p.idesc = make_q8_idesc(pair ? 256 : 128, p.tile_n);
+            p.per_stage = q8_per_stage(p.tile_n, pair);
+            // few rows: a box of 64 (what the products read behind it is not stored)
+            const bool low = !pair && p.M <= 64;
+            p.a_bytes = low ? 64 * 128 : 128 * 128;
+            const CUtensorMap &tmA = low ? rt->hmaps[li] : rt->tmaps[li];
             p.launch_id = (int)li;
             const ConvMaps &b = rt->conv[li];
             const CUtensorMap &tmB = p.tile_n == 32 ? b.a0 : p.tile_n == 64 ? b.a1 : b.o;
             const int tiles = p.m_tiles * p.n_tiles, smem = q8_smem_bytes(g.hw, p.tile_n, pair);
-            if (pair) le = to.pdl_cluster(xk::q8_tc_kernel<2>, 2 * std::min(tiles, std::max(1, sms / 2)), xk::kQ8Threads, smem, 2, rt->tmaps[li], tmB, p);
-            else le = to.pdl(xk::q8_tc_kernel<1>, std::min(tiles, sms), xk::kQ8Threads, smem, rt->tmaps[li], tmB, p);
+            if (pair) le = to.pdl_cluster(xk::q8_tc_kernel<2>, 2 * std::min(tiles, std::max(1, sms / 2)), xk::kQ8Threads, smem, 2, tmA, tmB, p);
+            else le = to.pdl(xk::q8_tc_kernel<1>, std::min(tiles, sms), xk::kQ8Threads, smem, tmA, tmB, p);
             break;
         }
         case LK_Q8_SMALL: {
@@ -739,9 +756,10 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
             p.x = ptr(L.in0); p.w = ws + L.w_off; p.ws = (const float *)(ws + L.w2_off); p.bias = (const float *)(ws + L.b_off); p.y = ptr(L.out);
             p.M = N * L.rows_per_image; p.N = L.K; p.K = L.C; p.pitch = L.q_pitch; p.act = L.act; p.out_f32 = L.out_dtype == XENOS_DTYPE_F32;
             p.vec = L.C % (L.row_in_f32 ? 4 : 8) == 0;
-            const int grid = (L.K + 15) / 16, smem = p.M * (L.q_pitch + 64);
-            if (L.row_in_f32) le = to.pdl(p.M <= 8 ? xk::q8_small_kernel<1, true> : xk::q8_small_kernel<2, true>, grid, 256, smem, p);
-            else le = to.pdl(p.M <= 8 ? xk::q8_small_kernel<1, false> : xk::q8_small_kernel<2, false>, grid, 256, smem, p);
+            const int grid = std::min((L.K + 15) / 16, 2 * sms), smem = p.M * (L.q_pitch + 64);
+            auto *k = L.row_in_f32 ? (p.M <= 8 ? xk::q8_small_kernel<1, true> : xk::q8_small_kernel<2, true>)
+                                   : (p.M <= 8 ? xk::q8_small_kernel<1, false> : xk::q8_small_kernel<2, false>);
+            le = to.pdl(k, grid, 256, smem, p);
             break;
         }
         case LK_LOGPROB: {
@@ -1070,7 +1088,7 @@ xenos_status_t runtime_bind(Graph &g, void *ws, void *stream_v, bool record) {
     to.optin = static_cast<Runtime *>(g.rt)->optin;
     // (any aligned address does for buffers that only a run names; some kernels have a form of their own for one image)
     const std::vector<void *> in(g.inputs.size(), ws), out(g.outputs.size(), ws);
-    for (int batch : {g.max_batch, 1}) {
+    for (int batch : {g.max_batch, std::min(g.max_batch, 8), 1}) {
         st = issue_pass(g, batch, in.data(), out.data(), to, [](size_t) -> xenos_status_t { return XENOS_OK; });
         if (st != XENOS_OK) return st;
     }

@@ -285,7 +285,7 @@ def test_norm_keeps_what_is_not_finite_in_its_row():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("rows,c", [(20001, 264), (9000, 512), (7500, 1000), (7301, 1024), (5003, 1032), (3700, 2048), (2500, 4000), (2400, 4096), (1300, 5000),
-                                    (1200, 8192), (700, 16384), (601, 12000)])
+                                    (1200, 8192), (700, 16384), (601, 12000), (9500, 257), (9501, 1023), (4800, 2047), (2401, 4095), (1203, 8191), (602, 16383)])
 def test_norm_of_many_rows(rows, c):
     """Enough rows for the CTAs that stay and walk over them; the last round of rows does not fill them."""
     for kind, out in (("bf16", "bf16"), ("f32", "f32")):
@@ -353,7 +353,7 @@ def check_q8(got, x, w, s, b, act, out):
 @pytest.mark.gpu
 @pytest.mark.parametrize("rows,c,n", [(1, 1, 1), (1, 16, 8), (1, 4096, 100), (2, 100, 33), (8, 128, 64), (8, 1111, 31), (9, 64, 17), (16, 1024, 1000),
                                       (16, 200, 1999), (17, 64, 32), (17, 1, 5), (100, 1000, 1000), (128, 128, 256), (129, 129, 257), (300, 1111, 1999),
-                                      (513, 320, 96), (40, 16500, 40), (5, 9000, 24)])
+                                      (513, 320, 96), (40, 16500, 40), (5, 9000, 24), (3, 512, 6001), (1, 16384, 4800)])
 def test_q8_matches_the_definition(rows, c, n):
     for kind, out, act, bias in (("bf16", "bf16", 0, True), ("f32", "f32", 1, False), ("bf16", "f32", 2, True), ("f32", "bf16", 0, False)):
         build, x, w, s, b = q8_case(rows, c, n, kind, out, act, bias, 0)
