@@ -10,8 +10,8 @@
 //   one CTA   tiles of 128 rows x 32..256 channels, for products whose larger tiles would leave SMs idle
 //   a pair    two CTAs of a cluster share a tile of 256 x 256 (cta_group::2): each brings its 128 rows of both operands, so a block of 128 deep
 //             takes 32 KB per SM for 512 cycles of the tensor pipe instead of 48 KB (L2 gives an SM some 75 bytes a cycle)
-// Results go through a 32-row box per warp in shared memory and leave as 16-byte pieces of rows; rows that are not whole pieces leave
-// element by element.
+// Results leave through 32-row boxes in shared memory by bulk tensor stores (16-byte pieces of rows stored by the threads: 4096 x 1024 x 16384 73.9 us
+// against 58 so); rows that are not whole 16-byte pieces leave element by element.
 //
 // q8_small_kernel (up to 16 rows): a pass over the weights, bound by their bytes.  A CTA owns 16 channels, its 8 warps share the
 // depth; mma.sync takes the channels as its 16 rows and the activation's rows as its 8 columns (tcgen05 has no shape that reads
@@ -38,6 +38,7 @@ struct Q8Params {
     int per_stage;                 // blocks of a stage: 2 where a tile is narrow
     uint32_t a_bytes;              // a box of the activation (its rows x 128)
     int act, out_f32, vec;         // vec: rows of the result are whole 16-byte pieces
+    int wide;                      // boxes of 64 channels of bf16 (else 32): 128 bytes a row either way where it counts
     int off_stage, off_par, off_bar;
     uint32_t idesc;
     int launch_id;
@@ -117,7 +118,7 @@ __device__ __forceinline__ Q8Tile q8_tile(const Q8Params &g, int ti) {
 
 template <int kPair>
 __global__ void __launch_bounds__(kQ8Threads, 1)
-q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ Q8Params g) {
+q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Q8Params g) {
     extern __shared__ uint8_t smem_raw[];
     pdl_launch_dependents();
     const uint32_t raw = smem_u32(smem_raw);
@@ -231,6 +232,9 @@ q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CU
         const int e = warp - 4, quarter = warp & 3, half = e >> 2;
         const uint32_t t_warp = tmem_base + ((uint32_t)(quarter * 32) << 16);
         uint8_t *box = sm + g.off_stage + e * 4096;
+        // the warp's s-th chunk of 32 columns: two warps of a quarter take turns, two chunks at a time where a box holds those
+        const bool wide = g.wide;
+        auto chunk = [&](int s) { return wide ? 4 * (s >> 1) + 2 * half + (s & 1) : half + 2 * s; };
         float *pars = reinterpret_cast<float *>(sm + g.off_par + e * 1024);
         const int chunks = g.tile_n / 32;
         int i = 0;
@@ -243,8 +247,8 @@ q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CU
             float wv[4], bv[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                const int x = t.nt * g.tile_n + (half + 2 * c) * 32 + lane;
-                const bool in = half + 2 * c < chunks && x < g.N;
+                const int x = t.nt * g.tile_n + chunk(c) * 32 + lane;
+                const bool in = chunk(c) < chunks && x < g.N;
                 wv[c] = in ? __ldg(g.ws + x) : 0.0f; bv[c] = in ? __ldg(g.bias + x) : 0.0f;
             }
             __syncwarp();                                        // (those of the tile before have been read)
@@ -253,12 +257,14 @@ q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CU
             if (!mbar_wait(accf_bar(b), (i >> 1) & 1)) { ok = false; break; }
             tc_fence_after();
 #pragma unroll 1
-            for (int j = half; j < chunks; j += 2) {
-                const int x0 = t.nt * g.tile_n + j * 32, x = x0 + lane;
-                const float *par = pars + (j >> 1) * 64;
+            for (int s = 0; chunk(s) < chunks; ++s) {
+                const int j = chunk(s), x0 = t.nt * g.tile_n + j * 32, x = x0 + lane;
+                const bool upper = wide && (s & 1);              // the right half of a box
+                const float *par = pars + s * 64;
                 float v[32];
                 tmem_ld32(t_warp + b * g.tile_n + j * 32, v);
-                __syncwarp();                                    // (the box of the chunk before has been read)
+                if (g.vec && !upper && elect_one()) bulk_wait_read<0>();      // the store that last left the box has read it
+                __syncwarp();
 #pragma unroll
                 for (int c = 0; c < 32; c += 4) {
                     const float4 w = *reinterpret_cast<const float4 *>(par + c), bb = *reinterpret_cast<const float4 *>(par + 32 + c);
@@ -276,32 +282,26 @@ q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CU
                     for (int c = 0; c < 8; ++c)
                         *reinterpret_cast<float4 *>(box + lane * 128 + ((c ^ (lane & 7)) << 4)) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
                 } else {
+                    const uint32_t row = wide ? lane * 128 : lane * 64, c0 = upper ? 4u : 0u, turn = wide ? lane & 7 : (lane >> 1) & 3;
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
-                        *reinterpret_cast<uint4 *>(box + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4)) =
+                        *reinterpret_cast<uint4 *>(box + row + (((c0 + c) ^ turn) << 4)) =
                             make_uint4(pack2(v[8 * c], v[8 * c + 1]), pack2(v[8 * c + 2], v[8 * c + 3]), pack2(v[8 * c + 4], v[8 * c + 5]), pack2(v[8 * c + 6], v[8 * c + 7]));
                 }
-                __syncwarp();
+                if (wide && !upper) continue;
                 if (g.vec) {
-                    if (g.out_f32) {
-#pragma unroll
-                        for (int r = lane >> 3; r < 32; r += 4) {
-                            const int c = lane & 7;
-                            if (m0 + r < g.M && x0 + c * 4 < g.N)
-                                *reinterpret_cast<float4 *>(static_cast<float *>(g.y) + (size_t)(m0 + r) * g.N + x0 + c * 4) =
-                                    *reinterpret_cast<const float4 *>(box + r * 128 + ((c ^ (r & 7)) << 4));
-                        }
-                    } else {
-#pragma unroll
-                        for (int r = lane >> 2; r < 32; r += 8) {
-                            const int c = lane & 3;
-                            if (m0 + r < g.M && x0 + c * 8 < g.N)
-                                *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(g.y) + (size_t)(m0 + r) * g.N + x0 + c * 8) =
-                                    *reinterpret_cast<const uint4 *>(box + r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
-                        }
-                    }
-                } else if (x < g.N) {
-                    for (int r = 0; r < 32 && m0 + r < g.M; ++r) {
+                    fence_proxy_async();
+                    __syncwarp();
+                    // (what reaches behind the last row or channel is not stored)
+                    if (elect_one()) { tma_store_2d(&tmO, smem_u32(box), upper ? x0 - 32 : x0, m0); bulk_commit(); }
+                    __syncwarp();
+                    continue;
+                }
+                __syncwarp();
+                if (x < g.N) {
+#pragma unroll 8
+                    for (int r = 0; r < 32; ++r) {
+                        if (m0 + r >= g.M) continue;
                         if (g.out_f32)
                             static_cast<float *>(g.y)[(size_t)(m0 + r) * g.N + x] = *reinterpret_cast<const float *>(box + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
                         else
@@ -314,6 +314,8 @@ q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CU
             __syncwarp();
             if (lane == 0) q8_arrive_first<kPair>(acce_bar(b));
         }
+        if (elect_one()) bulk_wait_read<0>();
+        __syncwarp();
         if (!ok && lane == 0) { *gave_up = 1; atomicCAS(g.status, 0u, word | (5u << 8)); }
     }
     tc_fence_before();

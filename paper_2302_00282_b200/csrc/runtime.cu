@@ -189,6 +189,20 @@ static xenos_status_t encode_bytes_map(const Graph &g, Runtime *rt, void *base, 
     return XENOS_OK;
 }
 
+// Result of the 8-bit product: rows of N elements in boxes of 32 rows x 32 or 64 channels, swizzled by the box's width.
+static xenos_status_t encode_result_map(const Graph &g, Runtime *rt, void *base, int N, long long rows, bool f32, int cols, CUtensorMap *out) {
+    const cuuint64_t es = f32 ? 4 : 2;
+    cuuint64_t dims[2] = {(cuuint64_t)N, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)N * es};
+    cuuint32_t box[2] = {(cuuint32_t)cols, 32u};
+    cuuint32_t estr[2] = {1u, 1u};
+    if (((uintptr_t)base & 15u) || (strides[0] & 15u)) return fail(g, XENOS_E_CUDA, "internal: an 8-bit product's result is not addressable by TMA");
+    CUresult r = rt->encode(out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                            (cuuint64_t)cols * es == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(g, XENOS_E_CUDA, "cuTensorMapEncodeTiled (8-bit product's result) failed with code " + std::to_string((int)r));
+    return XENOS_OK;
+}
+
 // Layer norm / rounding of rows: the smallest group and number of chunks that hold `n` channels, or the walk over memory.
 using RowKernel = void (*)(xk::RowParams);
 struct RowChoice { RowKernel kernel; int threads, rows; };
@@ -200,7 +214,8 @@ template <bool kIn32, int kOut, bool kNorm>
 static RowChoice row_choice(int n, bool vec) {
     if (n > 16384) return {xk::row_long_kernel<kIn32, kOut, kNorm>, 512, 1};
     if (!vec)
-        return n <= 128 ? row_odd_choice<8, 2, kIn32, kOut, kNorm>() : n <= 1024 ? row_odd_choice<32, 4, kIn32, kOut, kNorm>()
+        return n <= 128 ? row_odd_choice<8, 2, kIn32, kOut, kNorm>() : n <= 512 ? row_odd_choice<32, 2, kIn32, kOut, kNorm>()
+             : n <= 1024 ? row_odd_choice<32, 4, kIn32, kOut, kNorm>() : n <= 2048 ? row_odd_choice<128, 2, kIn32, kOut, kNorm>()
              : n <= 4096 ? row_odd_choice<128, 4, kIn32, kOut, kNorm>() : row_odd_choice<512, 4, kIn32, kOut, kNorm>();
     if (n <= 64) return row_choice<8, 1, kIn32, kOut, kNorm>();
     if (n <= 128) return row_choice<8, 2, kIn32, kOut, kNorm>();
@@ -746,9 +761,18 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
             p.launch_id = (int)li;
             const ConvMaps &b = rt->conv[li];
             const CUtensorMap &tmB = p.tile_n == 32 ? b.a0 : p.tile_n == 64 ? b.a1 : b.o;
+            // result boxes: only this run's rows
+            p.wide = p.vec && !p.out_f32 && p.tile_n >= 128;
+            CUtensorMap now;
+            const CUtensorMap *tmO = &tmB;
+            if (p.vec) {
+                xenos_status_t st = encode_result_map(g, rt, p.y, L.K, p.M, p.out_f32, p.wide ? 64 : 32, &now);
+                if (st != XENOS_OK) return st;
+                tmO = &now;
+            }
             const int tiles = p.m_tiles * p.n_tiles, smem = q8_smem_bytes(g.hw, p.tile_n, pair);
-            if (pair) le = to.pdl_cluster(xk::q8_tc_kernel<2>, 2 * std::min(tiles, std::max(1, sms / 2)), xk::kQ8Threads, smem, 2, tmA, tmB, p);
-            else le = to.pdl(xk::q8_tc_kernel<1>, std::min(tiles, sms), xk::kQ8Threads, smem, tmA, tmB, p);
+            if (pair) le = to.pdl_cluster(xk::q8_tc_kernel<2>, 2 * std::min(tiles, std::max(1, sms / 2)), xk::kQ8Threads, smem, 2, tmA, tmB, *tmO, p);
+            else le = to.pdl(xk::q8_tc_kernel<1>, std::min(tiles, sms), xk::kQ8Threads, smem, tmA, tmB, *tmO, p);
             break;
         }
         case LK_Q8_SMALL: {
