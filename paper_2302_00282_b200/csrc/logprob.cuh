@@ -468,15 +468,19 @@ logprob_kernel(const LogprobParams p) {
     if (t < p.k) p.part_key[slot * p.k + t] = sh.best[t];
     __syncthreads();
     if (t == 0) {
-        __threadfence();
-        sh.last = atomicAdd(p.arrived + row, 1u) == (unsigned)p.parts - 1;
+        // (releases what the barrier has put before it, and acquires what the other CTAs released)
+        unsigned before;
+        asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(p.arrived + row) : "memory");
+        sh.last = before == (unsigned)p.parts - 1;
         if (sh.last) p.arrived[row] = 0u;
     }
     __syncthreads();
     if (!sh.last) return;
-    __threadfence();
     // (every warp joins the sums by itself, a part a lane)
+    const int n = p.parts * p.k;
     const float4 f = lane < p.parts ? __ldcg(reinterpret_cast<const float4 *>(p.part_mst + (row * p.parts + lane) * 4)) : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+    for (int i = t; i < n; i += G) sh.list[i] = __ldcg(p.part_key + row * n + i);
+    if (t < kLpMaxTop) sh.best[t] = 0ull;
     LpSum all{f.x, f.y, f.z};
 #pragma unroll
     for (int s = 16; s >= 1; s >>= 1) m = fmaxf(s == 16 ? f.x : m, __shfl_xor_sync(0xffffffffu, s == 16 ? f.x : m, s));
@@ -484,9 +488,6 @@ logprob_kernel(const LogprobParams p) {
 #pragma unroll
     for (int s = 16; s >= 1; s >>= 1) { all.s += __shfl_xor_sync(0xffffffffu, all.s, s); all.t += __shfl_xor_sync(0xffffffffu, all.t, s); }
     all.m = m;
-    const int n = p.parts * p.k;
-    for (int i = t; i < n; i += G) sh.list[i] = __ldcg(p.part_key + row * n + i);
-    if (t < kLpMaxTop) sh.best[t] = 0ull;
     __syncthreads();
     lp_rank<G>(sh.list, n, p.k, sh.best, t);
     __syncthreads();
