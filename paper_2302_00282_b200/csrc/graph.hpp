@@ -308,11 +308,12 @@ inline int q8_tile_n(const xenos_hw_info_t &hw, long long rows, int N, int kbloc
         if (q8_cycles(rows, N, kblocks, units, tn) <= q8_cycles(rows, N, kblocks, units, best)) best = tn;
     return best;
 }
-// ... and of pairs of CTAs with tiles of 256 x 256.
+// ... and of pairs of CTAs with tiles of 256 x 256, whose results leave slower than their few blocks are multiplied (1024 x 512 x 8192: 14.6 us by
+// pairs, 12.5 by CTAs with 256 channels; 2048 x 4096 x 4096: 34.2 and 35.1).
 inline double q8_pair_cycles(long long rows, int N, int kblocks, int units) {
     const double tiles = (double)((rows + 255) / 256) * ((N + 255) / 256);
     const int pairs = units / 2 < 1 ? 1 : units / 2;
-    return (double)(long long)((tiles + pairs - 1) / pairs) * (kblocks * 540.0 + 1800.0) + 1500.0;
+    return (double)(long long)((tiles + pairs - 1) / pairs) * (kblocks * 540.0 + 3500.0) + 1500.0;
 }
 
 }  // namespace xenos

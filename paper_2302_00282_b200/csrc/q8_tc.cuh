@@ -27,6 +27,8 @@
 namespace xk {
 
 constexpr int kQ8Threads = 384, kQ8EpiWarps = 8, kQ8MaxStages = 8;
+// Registers as for more threads (128 instead of 168): a CTA then fits beside those of the row kernel that it follows, and sets itself up while they work.
+constexpr int kQ8RegThreads = 512;
 
 struct Q8Params {
     const float *xs;               // scale per row
@@ -117,7 +119,7 @@ __device__ __forceinline__ Q8Tile q8_tile(const Q8Params &g, int ti) {
 }
 
 template <int kPair>
-__global__ void __launch_bounds__(kQ8Threads, 1)
+__global__ void __launch_bounds__(kQ8RegThreads, 1)
 q8_tc_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmO, const __grid_constant__ Q8Params g) {
     extern __shared__ uint8_t smem_raw[];
     pdl_launch_dependents();

@@ -169,7 +169,7 @@ def test_plans_of_the_row_operators():
     g = _one(head, batch=17)
     assert [l["kind"] for l in g.plan()["launches"]] == ["rows", "rows", "q8"]
     # a large product is cut among pairs of CTAs, one of few tiles is not
-    big = lambda batch: [l for l in _one(lambda g, x: _q8(g, x, 256, 4096), c=256, batch=batch).plan()["launches"] if l["kind"] == "q8"][0]  # noqa: E731
+    big = lambda batch: [l for l in _one(lambda g, x: _q8(g, x, 4096, 4096), c=4096, batch=batch).plan()["launches"] if l["kind"] == "q8"][0]  # noqa: E731
     assert big(8192)["pair"] == 1 and big(8192)["tile_n"] == 256
     assert big(100)["pair"] == 0
     # scores for LOGPROB alone stay fp32: twice the bytes of a bf16 tensor
@@ -353,7 +353,7 @@ def check_q8(got, x, w, s, b, act, out):
 @pytest.mark.gpu
 @pytest.mark.parametrize("rows,c,n", [(1, 1, 1), (1, 16, 8), (1, 4096, 100), (2, 100, 33), (8, 128, 64), (8, 1111, 31), (9, 64, 17), (16, 1024, 1000),
                                       (16, 200, 1999), (17, 64, 32), (17, 1, 5), (100, 1000, 1000), (128, 128, 256), (129, 129, 257), (300, 1111, 1999),
-                                      (513, 320, 96), (40, 16500, 40), (5, 9000, 24), (3, 512, 6001), (1, 16384, 4800)])
+                                      (513, 320, 96), (600, 300, 520), (2100, 520, 2056), (1500, 130, 3001), (40, 16500, 40), (5, 9000, 24), (3, 512, 6001), (1, 16384, 4800)])
 def test_q8_matches_the_definition(rows, c, n):
     for kind, out, act, bias in (("bf16", "bf16", 0, True), ("f32", "f32", 1, False), ("bf16", "f32", 2, True), ("f32", "bf16", 0, False)):
         build, x, w, s, b = q8_case(rows, c, n, kind, out, act, bias, 0)
@@ -362,7 +362,7 @@ def test_q8_matches_the_definition(rows, c, n):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("rows,c,n", [(2048, 256, 4096), (3001, 1000, 2500), (2500, 4096, 2049)])
+@pytest.mark.parametrize("rows,c,n", [(2048, 4096, 4096), (3001, 2600, 2500), (2500, 4096, 2049)])
 def test_q8_by_pairs_of_ctas(rows, c, n):
     for kind, out in (("bf16", "bf16"), ("f32", "f32")):
         build, x, w, s, b = q8_case(rows, c, n, kind, out, 0, True, 1)
