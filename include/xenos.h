@@ -164,17 +164,17 @@ XENOS_API xenos_status_t xenos_graph_mark_output(xenos_graph_t *g, xenos_id_t te
  * XENOS_E_UNSUPPORTED otherwise) and QMATMUL, a tensor-core product, is refused (XENOS_E_UNSUPPORTED).  All three are per row: a NaN or an
  * infinity reaches the results of its row and of no other.  They have no explicit split (XENOS_E_BAD_SPLIT).
  *
- * LAYERNORM goes through xenos_graph_add_op: weight = gamma [c], bias = beta [c] or NULL, bn_eps > 0.  The variance is the mean of the
+ * LAYERNORM goes through xenos_graph_add_op: weight = gamma [c], bias = beta [c] or NULL, bn_eps > 0, cout = c or 0 (XENOS_E_SHAPE if another).  The variance is the mean of the
  * squared deviations.  LAYERNORM -> QMATMUL is a link: the normalised row leaves as 8-bit values with its scale.
  *
  * QMATMUL: y[n] = act(sx * scale[n] * sum_k q[k] weight[n][k] + bias[n]) with q = round(127 x / a), halves to even, a = max_k |x[k]|,
  * sx = a / 127 for every row by itself; a row of zeros gives act(bias), a row with a NaN or an infinity gives NaN.  The sum of
  * products is exact (c <= 131072).  Weights are constants, given either as weight_i8 [cout][c] with scale [cout], or as fp32 weight
  * [cout][c], which the library rounds the same way (scale NULL).  The result has cout channels; a RELU or RELU6 record behind it is fused.
- * Errors: XENOS_E_INVALID (NULL or non-finite parameter, both or neither weights), XENOS_E_SHAPE (cout < 1), XENOS_E_UNSUPPORTED
+ * Errors: XENOS_E_INVALID (NULL or non-finite parameter, both or neither weights), XENOS_E_SHAPE (cout < 1, c), XENOS_E_UNSUPPORTED
  * (c > 131072), at compile as above. */
 typedef struct {
-    int32_t cout, act;
+    int32_t c, cout, act;         /* c: channels of a row that the weights are for (XENOS_E_SHAPE if the input has others) */
     const float *weight;          /* [cout][c], or NULL */
     const int8_t *weight_i8;      /* [cout][c], or NULL */
     const float *scale;           /* [cout] with weight_i8, else NULL */
@@ -193,7 +193,8 @@ XENOS_API xenos_status_t xenos_graph_add_qmatmul(xenos_graph_t *g, const xenos_q
  *  - a score of -inf is masked: probability 0, never an alternative; missing alternatives have id -1 and log-probability -inf.
  *  - a row with nothing but -inf: log-probabilities -inf, entropy 0, ids -1.
  *  - a row with a NaN or +inf: log-probabilities and entropy NaN; a NaN is no alternative.
- * Errors: XENOS_E_INVALID (bad id, top out of range, labels that are no I32 input), XENOS_E_SHAPE (rows differ), at compile as above. */
+ * Errors: XENOS_E_INVALID (bad id, top out of range, labels that are no I32 input), XENOS_E_SHAPE (rows differ), XENOS_E_UNSUPPORTED (rows of more
+ * than 2^30 scores), at compile as above. */
 XENOS_API xenos_status_t xenos_graph_add_logprob(xenos_graph_t *g, xenos_id_t logits, xenos_id_t labels, int32_t top,
                                                  xenos_id_t out[4]);
 

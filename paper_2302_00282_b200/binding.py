@@ -45,7 +45,7 @@ class OpDesc(ctypes.Structure):
 
 
 class QmatmulDesc(ctypes.Structure):
-    _fields_ = [("cout", ctypes.c_int32), ("act", ctypes.c_int32), ("weight", _f32p), ("weight_i8", _i8p), ("scale", _f32p),
+    _fields_ = [("c", ctypes.c_int32), ("cout", ctypes.c_int32), ("act", ctypes.c_int32), ("weight", _f32p), ("weight_i8", _i8p), ("scale", _f32p),
                 ("bias", _f32p)]
 
 
@@ -147,6 +147,10 @@ class Graph:
             arrs.append(a)
             return a
         d.weight, d.bias = _fp(c32(weight)), _fp(c32(bias))
+        if kind == OP_LAYERNORM and weight is not None:
+            d.cout = arrs[0].size
+            if bias is not None and arrs[1].size != arrs[0].size:
+                raise ValueError("weight and bias of a layer norm have one value per channel")
         if bn is not None:
             d.bn_gamma, d.bn_beta, d.bn_mean, d.bn_var = (_fp(c32(x)) for x in bn)
         d.bn_eps = bn_eps
@@ -161,7 +165,7 @@ class Graph:
         if weight.ndim != 2:
             raise ValueError("weight must be a matrix [cout][c]")
         d = QmatmulDesc()
-        d.cout, d.act = weight.shape[0], act
+        d.cout, d.c, d.act = weight.shape[0], weight.shape[1], act
         if weight.dtype == np.int8:
             w = np.ascontiguousarray(weight)
             d.weight_i8 = w.ctypes.data_as(_i8p)

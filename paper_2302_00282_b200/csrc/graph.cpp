@@ -163,6 +163,7 @@ xenos_status_t infer_and_append(Graph &g, const xenos_op_desc_t &d, const int *i
     case XENOS_OP_LAYERNORM:
         if (!need_inputs(1)) return fail(g, XENOS_E_INVALID, "layernorm takes one input");
         if (!d.weight) return fail(g, XENOS_E_INVALID, "layernorm: weight is NULL");
+        if (d.cout != 0 && d.cout != x.c) return fail(g, XENOS_E_SHAPE, "layernorm: the parameters are for rows of another length");
         if (!finite_all(d.weight, x.c) || (d.bias && !finite_all(d.bias, x.c))) return fail(g, XENOS_E_INVALID, "layernorm: non-finite parameter");
         if (!(d.bn_eps > 0.0f) || !std::isfinite(d.bn_eps)) return fail(g, XENOS_E_INVALID, "layernorm: bn_eps must be positive");
         op.w.assign(d.weight, d.weight + x.c);
@@ -235,6 +236,7 @@ xenos_status_t append_qmatmul(Graph &g, const xenos_qmatmul_desc_t &d, int in, i
     if (const char *why = not_an_operand(g, in)) return fail(g, XENOS_E_UNSUPPORTED, std::string("add_qmatmul: ") + why);
     const Tensor x = g.tensors[in];
     if (d.cout < 1) return fail(g, XENOS_E_SHAPE, "add_qmatmul: cout must be positive");
+    if (d.c != x.c) return fail(g, XENOS_E_SHAPE, "add_qmatmul: the weights are for rows of another length");
     if ((d.weight != nullptr) == (d.weight_i8 != nullptr)) return fail(g, XENOS_E_INVALID, "add_qmatmul: give either weight or weight_i8");
     if ((d.scale != nullptr) != (d.weight_i8 != nullptr)) return fail(g, XENOS_E_INVALID, "add_qmatmul: scale goes with weight_i8");
     if (d.act != XENOS_ACT_NONE && d.act != XENOS_ACT_RELU && d.act != XENOS_ACT_RELU6) return fail(g, XENOS_E_INVALID, "add_qmatmul: unknown activation");
@@ -280,6 +282,7 @@ xenos_status_t append_logprob(Graph &g, int logits, int labels, int top, int *ou
     if (const char *why = not_an_operand(g, logits)) return fail(g, XENOS_E_UNSUPPORTED, std::string("add_logprob: ") + why);
     if (top < 0 || top > 32) return fail(g, XENOS_E_INVALID, "add_logprob: top must be 0..32");
     const Tensor x = g.tensors[logits];
+    if (x.c > 1 << 30) return fail(g, XENOS_E_UNSUPPORTED, "add_logprob: more than 2^30 scores in a row");
     int n_labels = 0;
     if (labels >= 0) {
         const Tensor &l = g.tensors[labels];
@@ -364,6 +367,9 @@ xenos_status_t compile_graph(Graph &g, int max_batch, int precision) {
             if (x.io_dtype != XENOS_DTYPE_F32 || (!x.is_vec && x.io_layout != XENOS_LAYOUT_NCHW))
                 return fail(g, XENOS_E_UNSUPPORTED, "fp32 graphs produce F32 NCHW outputs");
         } else {
+            if (x.is_vec && row_result(g, t))
+                for (int c : x.consumers)
+                    if (!is_row_op(g.ops[c].kind)) return fail(g, XENOS_E_UNSUPPORTED, "an F32 result is read by an operator that takes bf16");
             if (x.is_vec && x.io_dtype != XENOS_DTYPE_F32)
                 return fail(g, XENOS_E_UNSUPPORTED, "bf16 graphs produce vector outputs in F32");
             if (!x.is_vec && x.io_dtype == XENOS_DTYPE_F32 && x.io_layout == XENOS_LAYOUT_NHWC && row_result(g, t)) {

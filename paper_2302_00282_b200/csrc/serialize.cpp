@@ -169,6 +169,10 @@ xenos_status_t load_graph(Graph &g, const uint8_t *buf, size_t bytes, bool *comp
         const char *bad = ver < 2 || o.kind > XENOS_OP_LOGPROB || o.in.empty() ? "kind" : nullptr;
         if (!bad) {
             const size_t c = (size_t)g.tensors[o.in[0]].c, n = (size_t)std::max(o.cout, 0);
+            if (o.kind != XENOS_OP_LOGPROB) {
+                const Tensor &x = g.tensors[o.in[0]], &y = g.tensors[o.out];
+                if (o.in.size() != 1 || y.h != x.h || y.w != x.w || y.is_vec != x.is_vec || y.c != (o.kind == XENOS_OP_LAYERNORM ? x.c : o.cout)) bad = "shape";
+            }
             if (o.kind == XENOS_OP_LAYERNORM && (o.w.size() != c || (o.has_bias && o.bias.size() != c) || !(o.eps > 0.0f))) bad = "layernorm";
             if (o.kind == XENOS_OP_QMATMUL && (!n || c > 131072 || o.q.size() != n * c || o.gamma.size() != n || (o.has_bias && o.bias.size() != n))) bad = "qmatmul";
             if (o.kind == XENOS_OP_LOGPROB) {

@@ -89,6 +89,10 @@ def test_refusals_at_the_call():
     assert code(lambda: g.add_qmatmul(wide, np.ones((1, 131073), np.int8), np.ones(1))) == xb.E_UNSUPPORTED
     with pytest.raises(ValueError):
         g.add_qmatmul(x, w8, np.ones(3))
+    with pytest.raises(ValueError):
+        g.add_op(xb.OP_LAYERNORM, [x], weight=one, bias=one[:15])
+    assert code(lambda: g.add_op(xb.OP_LAYERNORM, [x], weight=one[:15])) == xb.E_SHAPE
+    assert code(lambda: g.add_qmatmul(x, w8[:, :15], s)) == xb.E_SHAPE
     assert code(lambda: g.add_logprob(x, None, -1)) == xb.E_INVALID
     assert code(lambda: g.add_logprob(x, None, 33)) == xb.E_INVALID
     assert code(lambda: g.add_logprob(x, x, 1)) == xb.E_INVALID                                          # labels that are no labels
@@ -152,6 +156,16 @@ def test_refusals_at_compile():
         g.mark_output(g.add_op(xb.OP_CONV, [y], cout=8, k=1, weight=np.ones((8, 64, 1, 1))), xb.DTYPE_BF16, xb.LAYOUT_NHWC)
         return y
     assert code(lambda: _one(f32_read_by_conv, out=xb.DTYPE_F32)) == xb.E_UNSUPPORTED
+
+    def f32_vector_read_by_fc(g, x):
+        y = _norm(g, g.add_op(xb.OP_POOL_GLOBAL_AVG, [x]))
+        g.mark_output(g.add_op(xb.OP_FC, [y], cout=8, k=1, weight=np.ones((8, 64))), xb.DTYPE_F32, xb.LAYOUT_NHWC)
+        return y
+    assert code(lambda: _one(f32_vector_read_by_fc, out=xb.DTYPE_F32)) == xb.E_UNSUPPORTED
+    # widths that the other bf16 operators do not take
+    odd = lambda kind, **kw: code(lambda: _one(lambda g, x: g.add_op(kind, [_q8(g, x, n=21)], **kw), h=2))  # noqa: E731
+    assert odd(xb.OP_CONV, cout=8, k=1, weight=np.ones((8, 21, 1, 1))) == xb.E_UNSUPPORTED
+    assert odd(xb.OP_POOL_MAX, k=1) == xb.E_UNSUPPORTED
     _one(f32_read_by_conv, out=xb.DTYPE_BF16)
 
 
@@ -168,6 +182,14 @@ def test_plans_of_the_row_operators():
     assert [c["kind"] for c in g.plan()["chains"]] == ["norm_qmatmul"]
     g = _one(head, batch=17)
     assert [l["kind"] for l in g.plan()["launches"]] == ["rows", "rows", "q8"]
+    # the link can be asked for where the rule would not make it
+    def explicit(g, x):
+        n = _norm(g, x)
+        y = _q8(g, n)
+        g.link([n, y])
+        return y
+    assert kinds(_one(explicit, batch=4)) == ["rows", "q8"]
+    assert code(lambda: _one(lambda g, x: (lambda y: (g.link([y, g.add_op(xb.OP_RELU, [y])]), y)[1])(_norm(g, x)))) in (xb.E_UNSUPPORTED, xb.E_NOT_LINKABLE)
     # a large product is cut among pairs of CTAs, one of few tiles is not
     big = lambda batch: [l for l in _one(lambda g, x: _q8(g, x, 4096, 4096), c=4096, batch=batch).plan()["launches"] if l["kind"] == "q8"][0]  # noqa: E731
     assert big(8192)["pair"] == 1 and big(8192)["tile_n"] == 256
@@ -702,6 +724,59 @@ def test_head_over_batches_streams_captures_images_and_the_built_in_scratch():
         r.g.run_builtin_scratch(200, [t.data_ptr() for t in ins], [o.data_ptr() for o in bufs], r.stream)
         for u, v in zip(r.read(bufs, 200), want):
             assert np.array_equal(u, v)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,c,mid", [(9, 264, 520), (40, 200, 333), (700, 512, 1000)])
+def test_two_products_in_a_row(rows, c, mid):
+    """norm -> product with ReLU -> norm -> product: both products' 8-bit rows lie in the same scratch."""
+    rng = rng_of("two", rows)
+    x = rounded(2 * rng.standard_normal((rows, c)), "bf16")
+    g1, g2 = (1 + 0.2 * rng.standard_normal(c)).astype(np.float32), (1 + 0.2 * rng.standard_normal(mid)).astype(np.float32)
+    w1, w2 = rng.integers(-127, 128, (mid, c)).astype(np.int8), rng.integers(-127, 128, (c, mid)).astype(np.int8)
+    s1, s2 = np.full(mid, 0.01, np.float32), np.full(c, 0.01, np.float32)
+
+    def build(upto):
+        def f(g):
+            t = g.add_input(xb.DTYPE_BF16, xb.LAYOUT_NHWC, c, 1, 1)
+            a = g.add_op(xb.OP_LAYERNORM, [t], weight=g1)
+            b = g.add_op(xb.OP_RELU, [g.add_qmatmul(a, w1, s1)])
+            d = g.add_op(xb.OP_LAYERNORM, [b], weight=g2)
+            y = g.add_qmatmul(d, w2, s2)
+            return [((a, c), (b, mid), (d, mid), (y, c))[upto] + ("bf16",)]
+        return f
+    ins = [to_device(x, "bf16")]
+    a, b, d, y = (Rows(build(i), rows).run(ins, rows)[0] for i in range(4))
+    check_norm(a, x, g1, np.zeros(c), "bf16")
+    check_q8(b, a, w1, s1, None, 1, "bf16")
+    check_norm(d, b, g2, np.zeros(mid), "bf16")
+    check_q8(y, d, w2, s2, None, 0, "bf16")
+    r = Rows(build(3), rows, link=True)
+    assert sum(ch["kind"] == "norm_qmatmul" for ch in r.g.plan()["chains"]) == (2 if rows > 16 else 0)
+    for _ in range(3):
+        assert np.array_equal(r.run(ins, rows)[0], y)
+
+
+@pytest.mark.gpu
+def test_batches_on_both_sides_of_the_kernels_rules():
+    """A recorded pass whose kernels change with the batch: many rows, few rows, many again."""
+    c, most = 4096, 2600
+    rng = rng_of("rules")
+    g1 = (1 + 0.2 * rng.standard_normal(c)).astype(np.float32)
+
+    def build(g):
+        t = g.add_input(xb.DTYPE_BF16, xb.LAYOUT_NHWC, c, 1, 1)
+        a = g.add_op(xb.OP_LAYERNORM, [t], weight=g1)
+        lp, ent, ids, tops = g.add_logprob(g.add_op(xb.OP_LAYERNORM, [a], weight=g1), None, 3)
+        return [(a, c, "f32"), (ent, 1, "f32"), (ids, 3, "i32"), (tops, 3, "f32")]
+    r = Rows(build, most)
+    for rows in (most, 30, 30, 30, most, most, 1, 1, 900, 900):
+        x = rounded(2 * rng.standard_normal((rows, c)), "bf16")
+        got = r.run([to_device(x, "bf16")], rows)
+        check_norm(got[0], x, g1, np.zeros(c), "f32")
+        z = oracle.layernorm(got[0], g1, np.zeros(c), 1e-5)
+        lp, ent, ids, tops = oracle.logprob(z, None, 3)
+        assert np.abs(got[1] - ent).max() < 1e-4 and np.abs(got[3] - tops).max() < 1e-4
 
 
 @pytest.mark.gpu
