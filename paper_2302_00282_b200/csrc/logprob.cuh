@@ -62,6 +62,18 @@ __device__ __forceinline__ LpSum lp_rebase(const LpSum &a, float to) {
     return a.m > -INFINITY || a.s != 0.0f ? LpSum{to, a.s * f, fmaf(a.s, d, a.t) * f} : LpSum{to, 0.0f, 0.0f};
 }
 
+// The sums of a warp's lanes joined, relative to the largest m (each has the result).
+__device__ __forceinline__ LpSum lp_join(LpSum a) {
+    float m = a.m;
+#pragma unroll
+    for (int s = 16; s >= 1; s >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, s));
+    a = lp_rebase(a, m > -INFINITY ? m : 0.0f);
+#pragma unroll
+    for (int s = 16; s >= 1; s >>= 1) { a.s += __shfl_xor_sync(0xffffffffu, a.s, s); a.t += __shfl_xor_sync(0xffffffffu, a.t, s); }
+    a.m = m;
+    return a;
+}
+
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
 // Adds 2^d and d 2^d, d = x log2(e) - c, of U chunks.
@@ -476,20 +488,42 @@ logprob_kernel(const LogprobParams p) {
     }
     __syncthreads();
     if (!sh.last) return;
-    // (every warp joins the sums by itself, a part a lane)
     const int n = p.parts * p.k;
-    const float4 f = lane < p.parts ? __ldcg(reinterpret_cast<const float4 *>(p.part_mst + (row * p.parts + lane) * 4)) : make_float4(-INFINITY, 0.0f, 0.0f, 0.0f);
+    LpSum all{-INFINITY, 0.0f, 0.0f};
+    if (t < p.parts) {
+        const float4 f = __ldcg(reinterpret_cast<const float4 *>(p.part_mst + (row * p.parts + t) * 4));
+        all = LpSum{f.x, f.y, f.z};
+    }
     for (int i = t; i < n; i += G) sh.list[i] = __ldcg(p.part_key + row * n + i);
     if (t < kLpMaxTop) sh.best[t] = 0ull;
-    LpSum all{f.x, f.y, f.z};
-#pragma unroll
-    for (int s = 16; s >= 1; s >>= 1) m = fmaxf(s == 16 ? f.x : m, __shfl_xor_sync(0xffffffffu, s == 16 ? f.x : m, s));
-    all = lp_rebase(all, m > -INFINITY ? m : 0.0f);
-#pragma unroll
-    for (int s = 16; s >= 1; s >>= 1) { all.s += __shfl_xor_sync(0xffffffffu, all.s, s); all.t += __shfl_xor_sync(0xffffffffu, all.t, s); }
-    all.m = m;
+    if (t == 0) sh.n = 0;
+    if (warp == 0) all = lp_join(all);
     __syncthreads();
-    lp_rank<G>(sh.list, n, p.k, sh.best, t);
+    const LpKey *from = sh.list;
+    int listed = n;
+    if (p.k && p.k <= p.parts) {
+        // The k-th best of the parts' first entries is a lower bound again, which only those k parts' entries reach: k * k at most.
+        // (Parts without an entry have 0 there, which no other is below; then fewer than k parts have any.)  Ranking all entries instead is a fifth of
+        // the whole chain: 7.6 against 6.5 us for the 8 best of one row of 131072 in 16 parts.
+        static_assert(G != 256 || kLpMaxParts * kLpMaxParts <= G, "the entries that reach the bound must fit");
+        if (warp == 0) {
+            const LpKey head = lane < p.parts ? sh.list[lane * p.k] : 0ull;
+            int before = 0;
+#pragma unroll
+            for (int q = 0; q < kLpMaxParts; ++q) before += __shfl_sync(0xffffffffu, head, q) > head;
+            const uint32_t at = __ballot_sync(0xffffffffu, head && before == p.k - 1);
+            if (at ? lane == __ffs(at) - 1 : lane == 0) sh.mk[0] = at ? head : 0ull;
+        }
+        __syncthreads();
+        const LpKey bound = sh.mk[0];
+        for (int i = t; i < n; i += G) {
+            const LpKey q = sh.list[i];
+            if (q && q >= bound) sh.key[atomicAdd(&sh.n, 1)] = q;
+        }
+        __syncthreads();
+        from = sh.key; listed = sh.n;
+    }
+    lp_rank<G>(from, listed, p.k, sh.best, t);
     __syncthreads();
     lp_finish<G, kIn32>(p, x, row, t, all, sh.best, lab0, x0);
 }

@@ -538,6 +538,27 @@ def test_logprob_ties_sorted_rows_and_plateaus(c):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("c", [17000, 24600, 65536, 131072])
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_logprob_rows_of_several_parts(c, kind):
+    """Two to sixteen CTAs share a row: as many answers as parts, fewer and more; parts without an entry, with all of the best, with equal ones."""
+    x, _ = lp_input(8, c, 0, 7)
+    sixteenth = c // 16
+    x[1, -40:] += 50                                            # the best are all in the last part
+    x[2] = -np.inf
+    x[2, ::3 * sixteenth] = 1.0                                 # fewer entries than answers, far apart
+    x[3] = 0.5
+    x[4, ::sixteenth] = 90.0                                    # equal best entries in every part
+    x[5] = np.linspace(4, -4, c)
+    x[6, sixteenth:] = -np.inf                                  # entries in the first part only
+    x[7, : c - 3] = -np.inf
+    x = rounded(x, kind)
+    dev = to_device(x, kind)
+    for top in (1, 2, 3, 4, 7, 8, 9, 15, 16, 17, 32):
+        check_lp(Rows(lp_build(c, kind, 0, top), 8).run([dev], 8), x, None, top)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("c", [8, 1003, 4001, 60000])
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 def test_logprob_masks_and_values_that_are_not_finite(c, kind):
