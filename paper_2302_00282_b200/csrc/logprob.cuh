@@ -503,8 +503,8 @@ logprob_kernel(const LogprobParams p) {
     int listed = n;
     if (p.k && p.k <= p.parts) {
         // The k-th best of the parts' first entries is a lower bound again, which only those k parts' entries reach: k * k at most.
-        // (Parts without an entry have 0 there, which no other is below; then fewer than k parts have any.)  Ranking all entries instead is a fifth of
-        // the whole chain: 7.6 against 6.5 us for the 8 best of one row of 131072 in 16 parts.
+        // (Parts without an entry have 0 there, which no other is below; then fewer than k parts have any.)  Ranking all entries instead: 7.1 against
+        // 6.5 us for the 8 best of one row of 131072 in 16 parts.
         static_assert(G != 256 || kLpMaxParts * kLpMaxParts <= G, "the entries that reach the bound must fit");
         if (warp == 0) {
             const LpKey head = lane < p.parts ? sh.list[lane * p.k] : 0ull;
