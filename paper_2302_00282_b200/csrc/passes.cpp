@@ -1731,8 +1731,6 @@ struct Lower {
         }
         if (g.chains[ci].split.user && (g.chains[ci].split.outc > 1 || g.chains[ci].split.h > 1 || g.chains[ci].split.w > 1 || g.chains[ci].split.k > 1))
             return fail(g, XENOS_E_BAD_SPLIT, "split: element-wise, pooling and depthwise kernels are split one vector per thread; no explicit split");
-        const Tensor &x = g.tensors[n.in[0]];
-        if (!x.is_vec && x.c % 8) return fail(g, XENOS_E_UNSUPPORTED, "bf16 NHWC tensors need a channel count that is a multiple of 8");
         if (n.kind == NK_DW) {
             if (n.k != 3) return fail(g, XENOS_E_UNSUPPORTED, "depthwise convolution: only 3x3 has a kernel");
             Launch L;
@@ -1841,9 +1839,25 @@ struct Lower {
     }
 };
 
+// What the kernels of operators that are no row operators read in a bf16 graph: 16-byte pieces of rows, so maps of whole chunks of
+// 8 channels (a convolution also reads an NCHW image, of any number of channels).
+static xenos_status_t check_operands(Graph &g) {
+    for (const Node &n : g.nodes) {
+        if (n.kind == NK_NORM || n.kind == NK_QMATMUL || n.kind == NK_LOGPROB) continue;
+        for (int t : n.in) {
+            const Tensor &x = g.tensors[t];
+            if (n.kind == NK_CONV && x.input_slot >= 0 && x.io_layout == XENOS_LAYOUT_NCHW) continue;
+            if (!x.is_vec && x.c % 8) return fail(g, XENOS_E_UNSUPPORTED, "bf16 NHWC tensors need a channel count that is a multiple of 8");
+        }
+    }
+    return XENOS_OK;
+}
+
 xenos_status_t split_and_lower(Graph &g) {
     g.launches.clear();
     g.param_blob.clear();
+    if (g.precision == XENOS_PRECISION_BF16_TENSOR)
+        if (xenos_status_t st = check_operands(g)) return st;
     Lower lw(g);
     for (int ci = 0; ci < (int)g.chains.size(); ++ci) {
         xenos_status_t st = lw.lower_chain(ci);
