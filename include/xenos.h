@@ -139,8 +139,8 @@ XENOS_API xenos_status_t xenos_graph_create(const xenos_hw_info_t *hw, xenos_gra
  * FP32_CUDA_CORE graphs take F32 NCHW; BF16_TENSOR graphs take F32 or BF16 NCHW when the
  * input feeds a convolution with fewer than 8 input channels (an image), BF16 NHWC with a
  * channel count that is a multiple of 8 otherwise.  Inputs that only row operators read may be
- * F32 or BF16 NHWC with any channel count (NCHW when h = w = 1, which is the same memory).  The labels of a LOGPROB
- * are I32 NHWC in either precision. */
+ * F32 or BF16 NHWC with any channel count (NCHW when h = w = 1, which is the same memory); compile refuses one that
+ * another operator reads as well (XENOS_E_UNSUPPORTED).  The labels of a LOGPROB are I32 NHWC in either precision. */
 XENOS_API xenos_status_t xenos_graph_add_input(xenos_graph_t *g, int32_t dtype, int32_t layout,
                                                int32_t c, int32_t h, int32_t w, xenos_id_t *tensor);
 
@@ -153,7 +153,8 @@ XENOS_API xenos_status_t xenos_graph_add_op(xenos_graph_t *g, const xenos_op_des
 /* Mark a tensor as a graph output.  The caller's buffer is dense: feature maps
  * [batch][C][H][W] (NCHW) or [batch][H][W][C] (NHWC), vectors [batch][C].
  * FP32 graphs: F32 NCHW.  BF16 graphs: vectors F32; feature maps BF16 NHWC; results of LAYERNORM and QMATMUL also F32
- * NHWC (only row operators of the graph may then read them too).  Results of LOGPROB: F32, ids I32, NHWC. */
+ * NHWC.  Operators of the graph may read its F32 outputs too if they are row operators (XENOS_E_UNSUPPORTED otherwise).  Results of
+ * LOGPROB: F32, ids I32, NHWC. */
 XENOS_API xenos_status_t xenos_graph_mark_output(xenos_graph_t *g, xenos_id_t tensor,
                                                  int32_t dtype, int32_t layout);
 

@@ -1839,14 +1839,16 @@ struct Lower {
     }
 };
 
-// What the kernels of operators that are no row operators read in a bf16 graph: 16-byte pieces of rows, so maps of whole chunks of
-// 8 channels (a convolution also reads an NCHW image, of any number of channels).
+// What the kernels of operators that are no row operators read in a bf16 graph: 16-byte pieces of bf16 rows, so NHWC maps of whole chunks of
+// 8 channels.  (A convolution also reads an NCHW image of either type, with any number of channels.)
 static xenos_status_t check_operands(Graph &g) {
     for (const Node &n : g.nodes) {
         if (n.kind == NK_NORM || n.kind == NK_QMATMUL || n.kind == NK_LOGPROB) continue;
         for (int t : n.in) {
             const Tensor &x = g.tensors[t];
             if (n.kind == NK_CONV && x.input_slot >= 0 && x.io_layout == XENOS_LAYOUT_NCHW) continue;
+            if (elem_dtype(g, t) != XENOS_DTYPE_BF16)
+                return fail(g, XENOS_E_UNSUPPORTED, "an F32 input, or an F32 output of the graph, is read by an operator that takes bf16 (row operators take either)");
             if (!x.is_vec && x.c % 8) return fail(g, XENOS_E_UNSUPPORTED, "bf16 NHWC tensors need a channel count that is a multiple of 8");
         }
     }

@@ -50,3 +50,66 @@ def test_concat_refuses_widths_that_are_not_whole_chunks(link):
         assert refusal(concat(order, 21), link=link) == xb.E_UNSUPPORTED
         g = compiled(concat(order, 24), link=link)
         assert [l["kind"] for l in g.plan()["launches"]].count("concat_part") == len(order)
+
+
+# ---- types -------------------------------------------------------------------------------------------------------------------
+def conv(g, x, n=64, c=64):
+    return g.add_op(xb.OP_CONV, [x], cout=n, k=1, weight=np.ones((n, c, 1, 1)))
+
+
+F32_READERS = {
+    "add": lambda g, x: (g.add_op(xb.OP_ADD, [norm(g, x), x]), B),
+    "add, other order": lambda g, x: (g.add_op(xb.OP_ADD, [x, norm(g, x)]), B),
+    "mul": lambda g, x: (g.add_op(xb.OP_MUL, [norm(g, x), x]), B),
+    "mac": lambda g, x: (g.add_op(xb.OP_MAC, [norm(g, x), norm(g, x), x]), B),
+    "concat": lambda g, x: (g.add_op(xb.OP_CONCAT, [norm(g, x), x]), B),
+    "split": lambda g, x: (g.add_op(xb.OP_SPLIT, [x], cout=8, pad=8), B),
+    "max pool": lambda g, x: (g.add_op(xb.OP_POOL_MAX, [x], k=2, stride=2), B),
+    "average pool": lambda g, x: (g.add_op(xb.OP_POOL_AVG, [x], k=2, stride=2), B),
+    "global pool": lambda g, x: (g.add_op(xb.OP_POOL_GLOBAL_AVG, [x]), F),
+    "convolution": lambda g, x: (conv(g, x), B),
+    "depthwise": lambda g, x: (g.add_op(xb.OP_CONV, [x], cout=64, k=3, pad=1, groups=64, weight=np.ones((64, 1, 3, 3))), B),
+    "shortcut": lambda g, x: (g.add_op(xb.OP_ADD, [conv(g, norm(g, x)), x]), B),
+    "shortcut convolution": lambda g, x: (g.add_op(xb.OP_ADD, [conv(g, norm(g, x)), conv(g, x)]), B),
+}
+
+
+@pytest.mark.parametrize("link", [False, True])
+@pytest.mark.parametrize("reader", F32_READERS)
+def test_f32_inputs_are_for_row_operators_alone(reader, link):
+    """A residual stream kept in 32 bits would be read as pairs of bf16 values."""
+    def build(dtype):
+        def f(g):
+            x = rows_in(g, dtype)
+            return [(norm(g, x), F), F32_READERS[reader](g, x)]
+        return f
+    assert refusal(build(F), link=link) == xb.E_UNSUPPORTED
+    compiled(build(B), link=link)
+
+
+def test_f32_inputs_of_row_operators_and_f32_images_stay():
+    def rows(g):
+        x = rows_in(g, F)
+        y = norm(g, x)
+        return [(product(g, x, n=24), F), (g.add_logprob(x)[1], F), (g.add_op(xb.OP_ADD, [y, norm(g, x)]), B)]
+    assert len(compiled(rows, link=True).plan()["launches"]) >= 5
+
+    def image(g):
+        x = g.add_input(F, xb.LAYOUT_NCHW, 3, 8, 8)
+        y = g.add_op(xb.OP_CONV, [x], cout=64, k=3, pad=1, weight=np.ones((64, 3, 3, 3)))
+        return [(norm(g, y), B)]
+    compiled(image, link=True)
+
+
+@pytest.mark.parametrize("link", [False, True])
+def test_f32_vector_outputs_are_read_by_row_operators_alone(link):
+    """A global average that is an output of the graph lies in the caller's memory as fp32; a fully connected layer reads bf16."""
+    def head(kind):
+        def build(g):
+            v = g.add_op(xb.OP_POOL_GLOBAL_AVG, [rows_in(g)])
+            y = g.add_op(xb.OP_FC, [v], cout=8, k=1, weight=np.ones((8, 64))) if kind == "fc" else product(g, v) if kind == "product" else norm(g, v)
+            return [(v, F), (y, F)]
+        return build
+    assert refusal(head("fc"), link=link) == xb.E_UNSUPPORTED
+    compiled(head("product"), link=link)
+    compiled(head("norm"), link=link)
