@@ -348,22 +348,29 @@ fc_small_kernel(const __nv_bfloat16 *__restrict__ x, const __nv_bfloat16 *__rest
     }
 }
 
+// Element-wise kernels take chunks of 8 elements; the last n % 8 (vectors need not be whole chunks) go to a thread each.
 __global__ void add_kernel(const __nv_bfloat16 *__restrict__ a, const __nv_bfloat16 *__restrict__ b,
-                           __nv_bfloat16 *__restrict__ y, long long n8, int act) {
-    for (long long i = blockIdx.x * (long long)blockDim.x + threadIdx.x; i < n8; i += (long long)gridDim.x * blockDim.x) {
+                           __nv_bfloat16 *__restrict__ y, long long n, int act) {
+    const long long first = blockIdx.x * (long long)blockDim.x + threadIdx.x, n8 = n >> 3;
+    for (long long i = first; i < n8; i += (long long)gridDim.x * blockDim.x) {
         f8 av = unpack8(reinterpret_cast<const uint4 *>(a)[i]);
         f8 bv = unpack8(reinterpret_cast<const uint4 *>(b)[i]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) av.v[j] = apply_act(av.v[j] + bv.v[j], act);
         reinterpret_cast<uint4 *>(y)[i] = pack8(av);
     }
+    if (first < (n & 7)) {
+        const long long e = n8 * 8 + first;
+        y[e] = __float2bfloat16_rn(apply_act(__bfloat162float(a[e]) + __bfloat162float(b[e]), act));
+    }
 }
 
 // x.mul (c == nullptr): a * b; x.mac: a * b + c.  The product is rounded to fp32 before the sum (no fused
 // multiply-add), as the operator-at-a-time definition has it.
 __global__ void mulmac_kernel(const __nv_bfloat16 *__restrict__ a, const __nv_bfloat16 *__restrict__ b,
-                              const __nv_bfloat16 *__restrict__ c, __nv_bfloat16 *__restrict__ y, long long n8) {
-    for (long long i = blockIdx.x * (long long)blockDim.x + threadIdx.x; i < n8; i += (long long)gridDim.x * blockDim.x) {
+                              const __nv_bfloat16 *__restrict__ c, __nv_bfloat16 *__restrict__ y, long long n) {
+    const long long first = blockIdx.x * (long long)blockDim.x + threadIdx.x, n8 = n >> 3;
+    for (long long i = first; i < n8; i += (long long)gridDim.x * blockDim.x) {
         f8 av = unpack8(reinterpret_cast<const uint4 *>(a)[i]);
         const f8 bv = unpack8(reinterpret_cast<const uint4 *>(b)[i]);
 #pragma unroll
@@ -374,6 +381,12 @@ __global__ void mulmac_kernel(const __nv_bfloat16 *__restrict__ a, const __nv_bf
             for (int j = 0; j < 8; ++j) av.v[j] = __fadd_rn(av.v[j], cv.v[j]);
         }
         reinterpret_cast<uint4 *>(y)[i] = pack8(av);
+    }
+    if (first < (n & 7)) {
+        const long long e = n8 * 8 + first;
+        float v = __fmul_rn(__bfloat162float(a[e]), __bfloat162float(b[e]));
+        if (c) v = __fadd_rn(v, __bfloat162float(c[e]));
+        y[e] = __float2bfloat16_rn(v);
     }
 }
 

@@ -113,3 +113,58 @@ def test_f32_vector_outputs_are_read_by_row_operators_alone(link):
     assert refusal(head("fc"), link=link) == xb.E_UNSUPPORTED
     compiled(head("product"), link=link)
     compiled(head("norm"), link=link)
+
+
+# ---- vectors of any width ----------------------------------------------------------------------------------------------------
+def picked(g, v, which, c=64):
+    """An 8-bit product that picks channels.  (Rows of small whole numbers and one 127 keep their values: the rows' scale is 1.)"""
+    w = np.zeros((len(which), c), np.int8)
+    w[np.arange(len(which)), which] = 1
+    return g.add_qmatmul(v, w, np.ones(len(which)))
+
+
+def whole_rows(batch, key, c=64):
+    rng = np.random.default_rng(key)
+    x = rng.integers(-15, 16, (batch, c)).astype(np.float64)
+    x[:, 0] = 127
+    return x
+
+
+def elementwise(kind, parts):
+    """In fp32, rounded after the product."""
+    a, b, *c = (p.astype(np.float32) for p in parts)
+    return np.maximum(a + b, 0) if kind == "add, relu" else a + b if kind == "add" else a * b if kind == "mul" else a * b + c[0]
+
+
+KINDS = {"add": (xb.OP_ADD, 2), "add, relu": (xb.OP_ADD, 2), "mul": (xb.OP_MUL, 2), "mac": (xb.OP_MAC, 3)}
+
+
+def vector_case(kind, n, batch, finish):
+    """finish(graph, element-wise result of vectors of n channels that products picked) -> results; the parts' values."""
+    code, operands = KINDS[kind]
+    which = [1 + (np.arange(n) * (3 + 2 * i) + i) % 63 for i in range(operands)]
+
+    def build(g):
+        v = g.add_op(xb.OP_POOL_GLOBAL_AVG, [g.add_input(B, xb.LAYOUT_NHWC, 64, 1, 1)])
+        parts = [picked(g, v, w) for w in which]
+        return finish(g, g.add_op(code, parts, act=xb.ACT_RELU if kind.endswith("relu") else xb.ACT_NONE))
+    x = whole_rows(batch, n * 100 + batch)
+    return build, x, elementwise(kind, [x[:, w] for w in which])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,batch", [(1, 1), (5, 1), (21, 1), (21, 3), (21, 8), (24, 3), (63, 7), (63, 33)])
+@pytest.mark.parametrize("kind", KINDS)
+def test_elementwise_vectors_of_any_width(kind, n, batch):
+    """Batch x width need not be whole chunks of 8: the last elements are computed, too (a workspace starts as NaN)."""
+    from row_util import Rows, rounded, to_device
+
+    def finish(g, y):
+        return [(g.add_qmatmul(y, np.eye(n, dtype=np.int8), np.ones(n)), n, "f32")]
+    build, x, want = vector_case(kind, n, batch, finish)
+    got, = Rows(build, batch).run([to_device(x, "bf16")], batch)
+    want = rounded(want, "bf16")
+    # the reader rounds each row to 127 steps of its largest magnitude: half a step, and the scale's rounding
+    step = np.abs(want).max(axis=1, keepdims=True) / 127
+    assert np.isfinite(got).all()
+    assert (np.abs(got - want) <= step * (0.5 + 127 * 4 * 2.0 ** -24)).all()
