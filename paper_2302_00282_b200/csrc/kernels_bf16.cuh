@@ -348,27 +348,42 @@ fc_small_kernel(const __nv_bfloat16 *__restrict__ x, const __nv_bfloat16 *__rest
     }
 }
 
-// Element-wise kernels take chunks of 8 elements; the last n % 8 (vectors need not be whole chunks) go to a thread each.
+// Element-wise kernels take chunks of 8 elements; the last n % 8 (vectors need not be whole chunks) go to a thread each.  kF32: the result is a
+// vector that leaves the graph.
+template <bool kF32>
+__device__ __forceinline__ void store_elements8(void *y, long long i, const f8 &v) {
+    if (kF32) {
+        float4 *o = static_cast<float4 *>(y) + 2 * i;
+        o[0] = make_float4(v.v[0], v.v[1], v.v[2], v.v[3]); o[1] = make_float4(v.v[4], v.v[5], v.v[6], v.v[7]);
+    } else static_cast<uint4 *>(y)[i] = pack8(v);
+}
+template <bool kF32>
+__device__ __forceinline__ void store_element(void *y, long long e, float v) {
+    if (kF32) static_cast<float *>(y)[e] = v;
+    else static_cast<__nv_bfloat16 *>(y)[e] = __float2bfloat16_rn(v);
+}
+template <bool kF32>
 __global__ void add_kernel(const __nv_bfloat16 *__restrict__ a, const __nv_bfloat16 *__restrict__ b,
-                           __nv_bfloat16 *__restrict__ y, long long n, int act) {
+                           void *__restrict__ y, long long n, int act) {
     const long long first = blockIdx.x * (long long)blockDim.x + threadIdx.x, n8 = n >> 3;
     for (long long i = first; i < n8; i += (long long)gridDim.x * blockDim.x) {
         f8 av = unpack8(reinterpret_cast<const uint4 *>(a)[i]);
         f8 bv = unpack8(reinterpret_cast<const uint4 *>(b)[i]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) av.v[j] = apply_act(av.v[j] + bv.v[j], act);
-        reinterpret_cast<uint4 *>(y)[i] = pack8(av);
+        store_elements8<kF32>(y, i, av);
     }
     if (first < (n & 7)) {
         const long long e = n8 * 8 + first;
-        y[e] = __float2bfloat16_rn(apply_act(__bfloat162float(a[e]) + __bfloat162float(b[e]), act));
+        store_element<kF32>(y, e, apply_act(__bfloat162float(a[e]) + __bfloat162float(b[e]), act));
     }
 }
 
 // x.mul (c == nullptr): a * b; x.mac: a * b + c.  The product is rounded to fp32 before the sum (no fused
 // multiply-add), as the operator-at-a-time definition has it.
+template <bool kF32>
 __global__ void mulmac_kernel(const __nv_bfloat16 *__restrict__ a, const __nv_bfloat16 *__restrict__ b,
-                              const __nv_bfloat16 *__restrict__ c, __nv_bfloat16 *__restrict__ y, long long n) {
+                              const __nv_bfloat16 *__restrict__ c, void *__restrict__ y, long long n) {
     const long long first = blockIdx.x * (long long)blockDim.x + threadIdx.x, n8 = n >> 3;
     for (long long i = first; i < n8; i += (long long)gridDim.x * blockDim.x) {
         f8 av = unpack8(reinterpret_cast<const uint4 *>(a)[i]);
@@ -380,13 +395,13 @@ __global__ void mulmac_kernel(const __nv_bfloat16 *__restrict__ a, const __nv_bf
 #pragma unroll
             for (int j = 0; j < 8; ++j) av.v[j] = __fadd_rn(av.v[j], cv.v[j]);
         }
-        reinterpret_cast<uint4 *>(y)[i] = pack8(av);
+        store_elements8<kF32>(y, i, av);
     }
     if (first < (n & 7)) {
         const long long e = n8 * 8 + first;
         float v = __fmul_rn(__bfloat162float(a[e]), __bfloat162float(b[e]));
         if (c) v = __fadd_rn(v, __bfloat162float(c[e]));
-        y[e] = __float2bfloat16_rn(v);
+        store_element<kF32>(y, e, v);
     }
 }
 

@@ -597,12 +597,14 @@ struct Lower {
         case NK_ADD:
             L.kind = f32 ? LK_F32_ADD : LK_ADD;
             L.in1 = n.in[1];
+            L.out_dtype = elem_dtype(g, n.out);
             break;
         case NK_MUL:
         case NK_MAC:
             L.kind = f32 ? LK_F32_MULMAC : LK_MULMAC;
             L.in1 = n.in[1];
             if (n.kind == NK_MAC) L.in2 = n.in[2];
+            L.out_dtype = elem_dtype(g, n.out);
             break;
         case NK_TRANSPOSE:
             L.kind = f32 ? LK_F32_TRANSPOSE : LK_TRANSPOSE;

@@ -684,7 +684,8 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
         case LK_ADD: {
             const Tensor &t = g.tensors[L.out];
             const long long n = (long long)N * (t.is_vec ? t.c : t.c * t.h * t.w);
-            le = to.plain(xk::add_kernel, ew_grid((n + 7) / 8, 256, sms), 256, 0, (const __nv_bfloat16 *)ptr(L.in0), (const __nv_bfloat16 *)ptr(L.in1), (__nv_bfloat16 *)ptr(L.out), n, L.act);
+            le = to.plain(L.out_dtype == XENOS_DTYPE_F32 ? xk::add_kernel<true> : xk::add_kernel<false>, ew_grid((n + 7) / 8, 256, sms), 256, 0,
+                (const __nv_bfloat16 *)ptr(L.in0), (const __nv_bfloat16 *)ptr(L.in1), ptr(L.out), n, L.act);
             break;
         }
         case LK_CONCAT_PART: {
@@ -695,8 +696,8 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
         case LK_MULMAC: {
             const Tensor &t = g.tensors[L.out];
             const long long n = (long long)N * (t.is_vec ? t.c : t.c * t.h * t.w);
-            le = to.plain(xk::mulmac_kernel, ew_grid((n + 7) / 8, 256, sms), 256, 0, (const __nv_bfloat16 *)ptr(L.in0), (const __nv_bfloat16 *)ptr(L.in1),
-                                                                         (const __nv_bfloat16 *)ptr(L.in2), (__nv_bfloat16 *)ptr(L.out), n);
+            le = to.plain(L.out_dtype == XENOS_DTYPE_F32 ? xk::mulmac_kernel<true> : xk::mulmac_kernel<false>, ew_grid((n + 7) / 8, 256, sms), 256, 0,
+                (const __nv_bfloat16 *)ptr(L.in0), (const __nv_bfloat16 *)ptr(L.in1), (const __nv_bfloat16 *)ptr(L.in2), ptr(L.out), n);
             break;
         }
         case LK_F32_MULMAC: {

@@ -168,3 +168,40 @@ def test_elementwise_vectors_of_any_width(kind, n, batch):
     step = np.abs(want).max(axis=1, keepdims=True) / 127
     assert np.isfinite(got).all()
     assert (np.abs(got - want) <= step * (0.5 + 127 * 4 * 2.0 ** -24)).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,batch", [(1, 1), (21, 3), (24, 5), (63, 33)])
+@pytest.mark.parametrize("kind", KINDS)
+def test_elementwise_vector_outputs_are_fp32(kind, n, batch):
+    """A vector output is F32 whatever operator it comes from: the sum or product of bf16 operands, not rounded again."""
+    from row_util import Rows, to_device
+    build, x, want = vector_case(kind, n, batch, lambda g, y: [(y, n, "f32")])
+    got, = Rows(build, batch).run([to_device(x, "bf16")], batch)
+    assert np.array_equal(got, want)
+
+
+@pytest.mark.gpu
+def test_residual_sum_of_a_vector_leaves_as_fp32():
+    """add(layernorm(v), v) is an output, and row operators read it as fp32."""
+    from row_util import Rows, assert_within, rounded, to_device
+    from oracle import rows as oracle
+    rng = np.random.default_rng(5)
+    x = rounded(rng.standard_normal((9, 64)) * 2, "bf16")
+
+    def build(outputs):
+        def f(g):
+            v = g.add_op(xb.OP_POOL_GLOBAL_AVG, [g.add_input(B, xb.LAYOUT_NHWC, 64, 1, 1)])
+            y = norm(g, v)
+            if not outputs:
+                return [(y, 64, "f32")]
+            s = g.add_op(xb.OP_ADD, [y, v])
+            return [(s, 64, "f32"), (norm(g, s), 64, "f32")]
+        return f
+    # (the layer norm's result as the add reads it: rounded to bf16, the same value as its fp32 output rounded here)
+    y, = Rows(build(False), 9).run([to_device(x, "bf16")], 9)
+    s, z = Rows(build(True), 9).run([to_device(x, "bf16")], 9)
+    assert np.array_equal(s, (rounded(y, "bf16").astype(np.float32) + x.astype(np.float32)).astype(np.float64))
+    want = oracle.layernorm(s, np.ones(64), np.zeros(64), 1e-5)
+    rstd = 1 / np.sqrt(s.var(axis=1, keepdims=True) + 1e-5)
+    assert_within(z, want, 2.0 ** -24 * np.abs(want) + 64 * 2.0 ** -24 * np.abs(s).max(axis=1, keepdims=True) * rstd)
