@@ -163,7 +163,8 @@ XENOS_API xenos_status_t xenos_graph_mark_output(xenos_graph_t *g, xenos_id_t te
  * In BF16_TENSOR graphs rows are bf16 or, as graph inputs and between row operators where noted, fp32; arithmetic is fp32.  In
  * FP32_CUDA_CORE graphs LAYERNORM and LOGPROB take tensors whose channels are contiguous (vectors, maps of one pixel;
  * XENOS_E_UNSUPPORTED otherwise) and QMATMUL, a tensor-core product, is refused (XENOS_E_UNSUPPORTED).  All three are per row: a NaN or an
- * infinity reaches the results of its row and of no other.  They have no explicit split (XENOS_E_BAD_SPLIT).
+ * infinity reaches the results of its row and of no other.  They have no explicit split (XENOS_E_BAD_SPLIT).  A tensor has at most 2^30 rows
+ * in a batch (XENOS_E_UNSUPPORTED at compile).
  *
  * LAYERNORM goes through xenos_graph_add_op: weight = gamma [c], bias = beta [c] or NULL, bn_eps > 0, cout = c or 0 (XENOS_E_SHAPE if another).  The variance is the mean of the
  * squared deviations.  LAYERNORM -> QMATMUL is a link: the normalised row leaves as 8-bit values with its scale.

@@ -25,7 +25,7 @@ struct Tensor {
     int output_slot = -1;         // >= 0: graph output number
     int io_dtype = XENOS_DTYPE_F32, io_layout = XENOS_LAYOUT_NCHW;   // for graph inputs / outputs
     int fixed = -1;               // >= 0: result of a LOGPROB, its type whatever the precision
-    int rows() const { return is_vec ? 1 : h * w; }
+    long long rows() const { return is_vec ? 1 : (long long)h * w; }      // of an image
 };
 
 struct Op {

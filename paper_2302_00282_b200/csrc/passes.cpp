@@ -1580,7 +1580,7 @@ struct Lower {
         const Tensor &x = g.tensors[t];
         const bool nchw = g.precision == XENOS_PRECISION_FP32_CUDA_CORE || (x.input_slot >= 0 && x.io_layout == XENOS_LAYOUT_NCHW);
         if (nchw && x.rows() > 1) return fail(g, XENOS_E_UNSUPPORTED, std::string(who) + ": rows of an NCHW tensor of more than one pixel are not contiguous");
-        if ((long long)g.max_batch * x.rows() > (1ll << 30)) return fail(g, XENOS_E_UNSUPPORTED, std::string(who) + ": more than 2^30 rows");
+        if (x.rows() > (1ll << 30) / g.max_batch) return fail(g, XENOS_E_UNSUPPORTED, std::string(who) + ": more than 2^30 rows");
         return XENOS_OK;
     }
     xenos_status_t no_split(int ci) {
@@ -1594,7 +1594,7 @@ struct Lower {
         Launch L;
         L.kind = LK_ROWS;
         L.in0 = t; L.C = L.K = x.c; L.H = x.h; L.W = x.w;
-        L.rows_per_image = x.rows();
+        L.rows_per_image = (int)x.rows();
         L.row_norm = norm != nullptr; L.row_out = out;
         L.row_in_f32 = elem_dtype(g, t) == XENOS_DTYPE_F32;
         if (norm) { L.w_off = put_f32(norm->w); L.b_off = put_f32(norm->b); L.eps = norm->eps; }
@@ -1630,7 +1630,7 @@ struct Lower {
         L.nodes = {ni};
         L.q_pitch = round_up(n.cin, 128);
         L.C = n.cin; L.K = n.cout; L.H = g.tensors[src].h; L.W = g.tensors[src].w;
-        L.rows_per_image = g.tensors[src].rows();
+        L.rows_per_image = (int)g.tensors[src].rows();
         L.act = n.act;
         L.out = n.out;
         L.out_dtype = elem_dtype(g, n.out);
@@ -1674,7 +1674,7 @@ struct Lower {
         L.kind = LK_LOGPROB;
         L.nodes = {ni};
         L.in0 = n.in[0]; L.C = L.K = x.c; L.H = x.h; L.W = x.w;
-        L.rows_per_image = x.rows();
+        L.rows_per_image = (int)x.rows();
         L.row_in_f32 = elem_dtype(g, n.in[0]) == XENOS_DTYPE_F32;
         L.top = n.top;
         if (n.in.size() > 1) { L.in1 = L.labels = n.in[1]; L.n_labels = g.tensors[n.in[1]].c; }

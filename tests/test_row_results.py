@@ -205,3 +205,12 @@ def test_residual_sum_of_a_vector_leaves_as_fp32():
     want = oracle.layernorm(s, np.ones(64), np.zeros(64), 1e-5)
     rstd = 1 / np.sqrt(s.var(axis=1, keepdims=True) + 1e-5)
     assert_within(z, want, 2.0 ** -24 * np.abs(want) + 64 * 2.0 ** -24 * np.abs(s).max(axis=1, keepdims=True) * rstd)
+
+
+# ---- numbers of rows ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("h,w,batch", [(65536, 65537, 1), (65536, 65536, 1), (46341, 46341, 3), (32769, 32768, 1), (32768, 16385, 2), (1 << 30, 3, 1)])
+def test_more_than_2_to_30_rows_are_refused(h, w, batch):
+    """Also where their number passes 32 bits: 65536 x 65537 rows are not 65536."""
+    for build in (lambda g, x: norm(g, x, 1), lambda g, x: product(g, x, 1, 1), lambda g, x: g.add_logprob(x)[1]):
+        assert refusal(lambda g: [(build(g, rows_in(g, F, 1, h, w)), F)], batch=batch) == xb.E_UNSUPPORTED
+    compiled(lambda g: [(norm(g, rows_in(g, F, 1, 32768, 32768 // batch), 1), F)], batch=batch)
