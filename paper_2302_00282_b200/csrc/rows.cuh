@@ -5,13 +5,14 @@
 //   to 8 bits  a = max |x|, q = round(127 x / a) (halves to even), scale = a / 127;  a = 0: q = 0
 //
 // Both are bound by HBM: the row is read once, kept in registers in its own type and written once.  A group of G threads owns a row, each thread V
-// chunks of 8 channels (one 16-byte access of bf16, two of fp32).  A warp or less takes rows of up to 4096 bf16 channels (2048 of fp32): no barrier, the
-// loads of a whole row under way at once, and warps that are at different points of their rows keep memory busy (4096 bf16 channels:
-// 128 threads with two barriers a row 55.8 us for 16384 rows).  Mean and squared deviations are two reductions over the registers, not the
+// chunks of 8 channels (one 16-byte access of bf16, two of fp32); the loads of a whole row are under way at once, and groups that are at different
+// points of their rows keep memory busy.  Mean and squared deviations are two reductions over the registers, not the
 // difference of two sums over memory, which would lose the digits of a variance that is small against the mean; the second one also sums
 // the deviations d, whose mean is the rounding of the first mean: (d - mean d) is exact to the last digits of d also for rows far from
 // zero.  The reductions of a group of several warps go through shared memory; gamma and beta come through L1, the row past it.
 // Rows that are not whole chunks (row_odd_kernel) are read and written channel by channel, a group's threads side by side.
+// The sums of a row have one order for each length, type and alignment, in every kernel here: that of columns of chunks (row_sum).  So a row's result
+// does not depend on the number of rows, and it is the same bit for bit where the link hands its 8-bit values to the product.
 #pragma once
 
 #include "gemm_tc.cuh"
@@ -92,23 +93,67 @@ __device__ __forceinline__ uint32_t row_reduce(uint32_t v, uint32_t *red, F f) {
     }
     return v;
 }
-template <int G>
-__device__ __forceinline__ float row_sum(float v, uint32_t *red) {
-    return __uint_as_float(row_reduce<G>(__float_as_uint(v), red, [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
-}
-template <int G>
-__device__ __forceinline__ float2 row_sum2(float a, float b, uint32_t *ra, uint32_t *rb) {
+// Sums over a row's G * A columns of chunks: a thread has A of them, column a G + t in v[a].  The order is that of G * A threads with one column each:
+// a tree over 32 columns, then their sums one after the other.
+// The tree over 32 lanes for one value, or for two: lanes that are 16 apart hand each other the one that they do not go on with, so two trees take as
+// many exchanges as one; lanes 0 to 15 have the first value's sum then, the others the second's.
+template <int A>
+__device__ __forceinline__ float row_trees(const float *v) {
+    static_assert(A == 1 || A == 2, "");
+    const bool up = A == 2 && (threadIdx.x & 16);
+    const float mine = up ? v[A - 1] : v[0], other = A == 1 || up ? v[0] : v[A - 1];
+    float x = mine + __shfl_xor_sync(0xffffffffu, other, 16);
 #pragma unroll
-    for (int s = (G < 32 ? G : 32) / 2; s >= 1; s >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, s); b += __shfl_xor_sync(0xffffffffu, b, s); }
-    if (G > 32) {
-        if ((threadIdx.x & 31) == 0) { ra[threadIdx.x >> 5] = __float_as_uint(a); rb[threadIdx.x >> 5] = __float_as_uint(b); }
+    for (int s = 8; s >= 1; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
+    return x;
+}
+// The sums of a warp's columns (G <= 32).
+template <int G, int A>
+__device__ __forceinline__ float row_columns(const float *v) {
+    static_assert(G <= 32 && (A == 1 || G * A == 32), "the columns of a row are one tree");
+    float x = v[0];
+    if (A == 2) x += v[A - 1];
+#pragma unroll
+    for (int s = G / 2; s >= 1; s >>= 1) x += __shfl_xor_sync(0xffffffffu, x, s);
+    return x;
+}
+// ... of several warps', left in shared memory, and their sum.
+template <int G, int A>
+__device__ __forceinline__ void row_leave(const float *v, uint32_t *red) {
+    const float x = row_trees<A>(v);
+    const int lane = threadIdx.x & 31;
+    if (lane % (32 / A) == 0) red[lane / (32 / A) * (G / 32) + (threadIdx.x >> 5)] = __float_as_uint(x);
+}
+template <int N>
+__device__ __forceinline__ float row_left(const uint32_t *red) {
+    float r = __uint_as_float(red[0]);
+#pragma unroll
+    for (int w = 1; w < N; ++w) r += __uint_as_float(red[w]);
+    return r;
+}
+template <int G, int A>
+__device__ __forceinline__ float row_sum(const float *v, uint32_t *red) {
+    if constexpr (G <= 32) return row_columns<G, A>(v);
+    else {
+        row_leave<G, A>(v, red);
         __syncthreads();
-        a = __uint_as_float(ra[0]); b = __uint_as_float(rb[0]);
-#pragma unroll
-        for (int w = 1; w < G / 32; ++w) { a += __uint_as_float(ra[w]); b += __uint_as_float(rb[w]); }
+        return row_left<G / 32 * A>(red);
     }
-    return make_float2(a, b);
 }
+template <int G>
+__device__ __forceinline__ float row_sum(float v, uint32_t *red) { return row_sum<G, 1>(&v, red); }
+// ... of two values, behind one barrier.
+template <int G, int A>
+__device__ __forceinline__ float2 row_sum2(const float *x, const float *y, uint32_t *rx, uint32_t *ry) {
+    if constexpr (G <= 32) return make_float2(row_columns<G, A>(x), row_columns<G, A>(y));
+    else {
+        row_leave<G, A>(x, rx); row_leave<G, A>(y, ry);
+        __syncthreads();
+        return make_float2(row_left<G / 32 * A>(rx), row_left<G / 32 * A>(ry));
+    }
+}
+template <int G>
+__device__ __forceinline__ float2 row_sum2(float a, float b, uint32_t *ra, uint32_t *rb) { return row_sum2<G, 1>(&a, &b, ra, rb); }
 template <int G>
 __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t *red) {
     return row_reduce<G>(v, red, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
@@ -194,9 +239,10 @@ __device__ __forceinline__ void row_quant8(const RowParams &p, long long row, in
     *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(p.y) + row * p.pitch + c) = make_uint2(row_bytes4(q[0], q[1], q[2], q[3]), row_bytes4(q[4], q[5], q[6], q[7]));
 }
 
-// Rows of whole chunks (channels a multiple of 8).
-template <int G, int V, bool kIn32, int kOut, bool kNorm>
-__global__ void __launch_bounds__(RowShape<G, V>::threads)
+// Rows of whole chunks (channels a multiple of 8).  A: columns whose sums a thread keeps apart (row_sum), chunk v being of column v % A.  (Linked norms with
+// two columns of four chunks are held to the registers of seven CTAs of 128 threads: 8192 rows of 512 fp32 13.6 us for 11.9 without that.)
+template <int G, int V, int A, bool kIn32, int kOut, bool kNorm>
+__global__ void __launch_bounds__(RowShape<G, V>::threads, kNorm && kOut == RO_Q8 && V == 4 && A == 2 ? 896 / RowShape<G, V>::threads : 0)
 row_kernel(const RowParams p) {
     typedef RowShape<G, V> Shape;
     constexpr int R = Shape::per_group, W = kIn32 ? 2 : 1;          // rows of a group; 16-byte words of a chunk
@@ -221,34 +267,45 @@ row_kernel(const RowParams p) {
         const float inv = 1.0f / (float)p.C;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            f32x2 s0 = 0ull, s1 = 0ull;                                // (zeros outside the row)
+            f32x2 s0[A] = {}, s1[A] = {};                              // (zeros outside the row)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 f32x2 e[4];
                 row_pairs<kIn32>(u[r][v], e);
-                s0 = add2(s0, add2(e[0], e[1])); s1 = add2(s1, add2(e[2], e[3]));
+                s0[v % A] = add2(s0[v % A], add2(e[0], e[1])); s1[v % A] = add2(s1[v % A], add2(e[2], e[3]));
             }
-            float a, b;
-            split2(add2(s0, s1), a, b);
-            const float mu = __fdiv_rn(row_sum<G>(a + b, red[0]), (float)p.C);
+            float sum[A];
+#pragma unroll
+            for (int a = 0; a < A; ++a) {
+                float x, y;
+                split2(add2(s0[a], s1[a]), x, y);
+                sum[a] = x + y;
+            }
+            const float mu = __fdiv_rn(row_sum<G, A>(sum, red[0]), (float)p.C);
             nmu[r] = pair2(-mu, -mu);
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            f32x2 s0 = 0ull, s1 = 0ull, q0 = 0ull, q1 = 0ull;
+            f32x2 s0[A] = {}, s1[A] = {}, q0[A] = {}, q1[A] = {};
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if ((v * G + t) * 8 >= p.C) continue;
+                const int a = v % A;
                 f32x2 e[4];
                 row_pairs<kIn32>(u[r][v], e);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) e[i] = add2(e[i], nmu[r]);
-                q0 = add2(q0, add2(e[0], e[1])); q1 = add2(q1, add2(e[2], e[3]));
-                s0 = fma2(e[0], e[0], s0); s1 = fma2(e[1], e[1], s1); s0 = fma2(e[2], e[2], s0); s1 = fma2(e[3], e[3], s1);
+                q0[a] = add2(q0[a], add2(e[0], e[1])); q1[a] = add2(q1[a], add2(e[2], e[3]));
+                s0[a] = fma2(e[0], e[0], s0[a]); s1[a] = fma2(e[1], e[1], s1[a]); s0[a] = fma2(e[2], e[2], s0[a]); s1[a] = fma2(e[3], e[3], s1[a]);
             }
-            float a, b, c, d;
-            split2(add2(s0, s1), a, b); split2(add2(q0, q1), c, d);
-            const float2 f = row_sum2<G>(a + b, c + d, red[1], red[2]);
+            float squares[A], rest[A];
+#pragma unroll
+            for (int a = 0; a < A; ++a) {
+                float x, y, z, w;
+                split2(add2(s0[a], s1[a]), x, y); split2(add2(q0[a], q1[a]), z, w);
+                squares[a] = x + y; rest[a] = z + w;
+            }
+            const float2 f = row_sum2<G, A>(squares, rest, red[1], red[2]);
             const float off = f.y * inv, rstd = rsqrtf(fmaxf(fmaf(f.x, inv, -off * off), 0.0f) + p.eps);
             rs[r] = pair2(rstd, rstd); noff[r] = pair2(-off * rstd, -off * rstd);
         }
@@ -400,18 +457,21 @@ row_stream_kernel(const RowParams p) {
     if (dead) for (int i = 0; i < 64; ++i) __nanosleep(1000);      // (time for copies under way)
 }
 
-// Any rows, one a group: a thread's channels are G apart, or four together where they leave as 8-bit values (a word of them).
+// Any rows, one a group: a thread's channels are G apart, so that sums have the order of row_stream_odd_kernel.  Rows that are only rounded to 8 bits
+// have no sums; there a thread takes four channels together, a word of the result.  (Linked norms are held to the registers of so many CTAs: 8192 rows of 4095
+// 80 us with the 106 registers that they would take, 60 with 80.)
 template <int G, int V, bool kIn32, int kOut, bool kNorm>
-__global__ void __launch_bounds__(G <= 32 ? 128 : G)
+__global__ void __launch_bounds__(G <= 32 ? 128 : G, kOut == RO_Q8 && kNorm ? (G <= 32 ? (V == 2 ? 8 : 5) : V == 2 ? 10 : G == 512 ? 2 : 768 / G) : 0)
 row_odd_kernel(const RowParams p) {
     constexpr int per_cta = G <= 32 ? 128 / G : 1;
+    constexpr bool words = kOut == RO_Q8 && !kNorm;
     __shared__ uint32_t red[4][32];
     pdl_launch_dependents();
     pdl_wait();
     const int t = threadIdx.x % G;
     const long long row = (long long)blockIdx.x * per_cta + threadIdx.x / G;
     const bool live = row < p.rows;
-    auto col = [&](int i) { return kOut == RO_Q8 ? ((i >> 2) * G + t) * 4 + (i & 3) : i * G + t; };
+    auto col = [&](int i) { return words ? ((i >> 2) * G + t) * 4 + (i & 3) : i * G + t; };
     float x[8 * V];
 #pragma unroll
     for (int i = 0; i < 8 * V; ++i)
@@ -446,15 +506,26 @@ row_odd_kernel(const RowParams p) {
 #pragma unroll
         for (int i = 0; i < 8 * V; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
         const RowScale sc = row_scale(row_max<G>(m, red[3]));
-        if (!live) return;
-        if (t == 0) p.scale[row] = sc.scale;
+        if (live && t == 0) p.scale[row] = sc.scale;
+        uint32_t *to = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(p.y) + row * p.pitch);      // (the pitch is a multiple of 128)
+        // channels G apart: four threads with four channels each exchange halves, then bytes, and each has four channels that lie together
+        const bool up2 = t & 2, up1 = t & 1;
 #pragma unroll
         for (int i = 0; i < 8 * V; i += 4) {
             uint32_t q[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) q[k] = row_quant<kIn32 && !kNorm>(x[i + k], sc);
+            uint32_t w = row_bytes4(q[0], q[1], q[2], q[3]);
+            int at = col(i);
+            if (!words) {
+                const uint32_t far2 = __shfl_xor_sync(0xffffffffu, w, 2);
+                w = up2 ? __byte_perm(far2, w, 0x7632) : __byte_perm(w, far2, 0x5410);
+                const uint32_t far1 = __shfl_xor_sync(0xffffffffu, w, 1);
+                w = up1 ? __byte_perm(far1, w, 0x7351) : __byte_perm(w, far1, 0x6240);
+                at = (i + (t & 3)) * G + (t & ~3);
+            }
             // (rows are filled up to the pitch with zeros: x = 0 there)
-            if (col(i) < p.pitch) *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(p.y) + row * p.pitch + col(i)) = row_bytes4(q[0], q[1], q[2], q[3]);
+            if (live && at < p.pitch) to[at / 4] = w;
         }
         return;
     }
@@ -471,7 +542,7 @@ row_odd_kernel(const RowParams p) {
 // Layer norm of many rows of any length, as row_stream_kernel: a thread's channels are G apart, so that gamma and beta stay in registers whatever the
 // rows' alignment; the copy engine brings the 16-byte pieces that a row meets, its neighbours' ends with them, but nothing behind the tensor (the
 // last row's end is read from where it is).
-template <int G, int V, bool kIn32, int kOut>
+template <int G, int V, int A, bool kIn32, int kOut>
 __global__ void __launch_bounds__(G, 512 / G)
 row_stream_odd_kernel(const RowParams p) {
     constexpr int S = 2, ES = kIn32 ? 4 : 2, N = 8 * V;
@@ -530,20 +601,21 @@ row_stream_odd_kernel(const RowParams p) {
                 if (c >= came && c < p.C) x[i] = kIn32 ? ld_scalar(static_cast<const float *>(p.x) + row * p.C + c) : ld_scalar(static_cast<const __nv_bfloat16 *>(p.x) + row * p.C + c);
             }
         }
-        float a = 0.0f, e = 0.0f;
+        float a[A] = {}, e[A] = {};          // (sums of columns, as row_kernel has them)
 #pragma unroll
-        for (int i = 0; i < N; ++i) a += x[i];
-        const float mu = __fdiv_rn(row_sum<G>(a, red[0]), (float)p.C);
+        for (int i = 0; i < N; ++i) a[i % A] += x[i];
+        const float mu = __fdiv_rn(row_sum<G, A>(a, red[0]), (float)p.C);
         ask(row + (long long)S * gridDim.x, s);
         if (++s == S) { s = 0; ph ^= 1u; }
-        a = 0.0f;
+#pragma unroll
+        for (int i = 0; i < A; ++i) a[i] = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             x[i] = i * G + t < p.C ? x[i] - mu : 0.0f;
-            e += x[i];
-            a = fmaf(x[i], x[i], a);
+            e[i % A] += x[i];
+            a[i % A] = fmaf(x[i], x[i], a[i % A]);
         }
-        const float2 f = row_sum2<G>(a, e, red[1], red[2]);
+        const float2 f = row_sum2<G, A>(a, e, red[1], red[2]);
         const float off = f.y * inv, rstd = rsqrtf(fmaxf(fmaf(f.x, inv, -off * off), 0.0f) + p.eps);
 #pragma unroll
         for (int i = 0; i < N; ++i) {

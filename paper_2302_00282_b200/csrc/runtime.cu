@@ -206,26 +206,43 @@ static xenos_status_t encode_result_map(const Graph &g, Runtime *rt, void *base,
 // Layer norm / rounding of rows: the smallest group and number of chunks that hold `n` channels, or the walk over memory.
 using RowKernel = void (*)(xk::RowParams);
 struct RowChoice { RowKernel kernel; int threads, rows; };
-template <int G, int V, bool kIn32, int kOut, bool kNorm>
-static RowChoice row_choice() { return {xk::row_kernel<G, V, kIn32, kOut, kNorm>, xk::RowShape<G, V>::threads, xk::RowShape<G, V>::rows}; }
+template <int G, int V, int A, bool kIn32, int kOut, bool kNorm>
+static RowChoice row_choice() { return {xk::row_kernel<G, V, A, kIn32, kOut, kNorm>, xk::RowShape<G, V>::threads, xk::RowShape<G, V>::rows}; }
 template <int G, int V, bool kIn32, int kOut, bool kNorm>
 static RowChoice row_odd_choice() { return {xk::row_odd_kernel<G, V, kIn32, kOut, kNorm>, G <= 32 ? 128 : G, G <= 32 ? 128 / G : 1}; }
+// A layer norm's columns (G x A) are those of the kernels for many rows (stream_choice), so that a row's sums have one order.  Which groups share them,
+// us: 2300 rows of 4096 bf16 11.4 by 128 threads, 12.9 by 64 with twice the chunks; 3000 of 2048 7.9 by 64, 9.2 by 32; 1000 of 8192 11.5 by 256, 12.9 by
+// 128; fp32: 2000 of 1024 5.7 by 64, 7.7 by 32.  A linked norm has a third reduction a row, which groups of fewer threads hide better: 8192 rows of 8192 bf16
+// 79.3 by 128 threads, 84.0 by 256; 4096 of 16384 96.5 by 256, 136 by 512; fp32: 8192 of 4096 47.4 by 128, 53.5 by 256 (each with the product of 24 channels behind).
+// Largest magnitudes have no order: rows that are only rounded are dealt to groups by themselves.
 template <bool kIn32, int kOut, bool kNorm>
 static RowChoice row_choice(int n, bool vec) {
+    constexpr bool link = kOut == xk::RO_Q8;
     if (n > 16384) return {xk::row_long_kernel<kIn32, kOut, kNorm>, 512, 1};
-    if (!vec)
-        return n <= 128 ? row_odd_choice<8, 2, kIn32, kOut, kNorm>() : n <= 512 ? row_odd_choice<32, 2, kIn32, kOut, kNorm>()
-             : n <= 1024 ? row_odd_choice<32, 4, kIn32, kOut, kNorm>() : n <= 2048 ? row_odd_choice<128, 2, kIn32, kOut, kNorm>()
-             : n <= 4096 ? row_odd_choice<128, 4, kIn32, kOut, kNorm>() : row_odd_choice<512, 4, kIn32, kOut, kNorm>();
-    if (n <= 64) return row_choice<8, 1, kIn32, kOut, kNorm>();
-    if (n <= 128) return row_choice<8, 2, kIn32, kOut, kNorm>();
-    if (n <= 256) return row_choice<8, 4, kIn32, kOut, kNorm>();
-    if (n <= 512) return row_choice<16, 4, kIn32, kOut, kNorm>();
-    if (n <= 1024) return row_choice<32, 4, kIn32, kOut, kNorm>();
-    if (n <= 2048) return row_choice<32, 8, kIn32, kOut, kNorm>();
-    if (n <= 4096) return kIn32 ? row_choice<128, 4, kIn32, kOut, kNorm>() : row_choice<64, 8, kIn32, kOut, kNorm>();
-    if (n <= 8192) return row_choice<128, 8, kIn32, kOut, kNorm>();
-    return row_choice<256, 8, kIn32, kOut, kNorm>();
+    if (!vec) {
+        if (n <= 1024) return n <= 128 ? row_odd_choice<8, 2, kIn32, kOut, kNorm>() : n <= 512 ? row_odd_choice<32, 2, kIn32, kOut, kNorm>() : row_odd_choice<32, 4, kIn32, kOut, kNorm>();
+        if constexpr (kNorm && !kIn32)
+            return n <= 2048 ? row_odd_choice<128, 2, kIn32, kOut, kNorm>() : n <= 4096 ? row_odd_choice<128, 4, kIn32, kOut, kNorm>()
+                 : n <= 8192 ? row_odd_choice<256, 4, kIn32, kOut, kNorm>() : row_odd_choice<512, 4, kIn32, kOut, kNorm>();
+        else
+            return n <= 2048 ? row_odd_choice<128, 2, kIn32, kOut, kNorm>() : n <= 4096 ? row_odd_choice<128, 4, kIn32, kOut, kNorm>() : row_odd_choice<512, 4, kIn32, kOut, kNorm>();
+    }
+    if (n <= 64) return row_choice<8, 1, 1, kIn32, kOut, kNorm>();
+    if (n <= 128) return row_choice<8, 2, 1, kIn32, kOut, kNorm>();
+    if (n <= 256) return row_choice<8, 4, 1, kIn32, kOut, kNorm>();
+    if constexpr (!kNorm) {
+        return n <= 512 ? row_choice<16, 4, 1, kIn32, kOut, kNorm>() : n <= 1024 ? row_choice<32, 4, 1, kIn32, kOut, kNorm>() : n <= 2048 ? row_choice<32, 8, 1, kIn32, kOut, kNorm>()
+             : n <= 4096 ? (kIn32 ? row_choice<128, 4, 1, kIn32, kOut, kNorm>() : row_choice<64, 8, 1, kIn32, kOut, kNorm>())
+             : n <= 8192 ? row_choice<128, 8, 1, kIn32, kOut, kNorm>() : row_choice<256, 8, 1, kIn32, kOut, kNorm>();
+    } else if constexpr (kIn32) {
+        return n <= 512 ? row_choice<link ? 16 : 32, link ? 4 : 2, link ? 2 : 1, kIn32, kOut, kNorm>() : n <= 1024 ? row_choice<64, 2, 1, kIn32, kOut, kNorm>()
+             : n <= 2048 ? row_choice<128, 2, 1, kIn32, kOut, kNorm>() : n <= 4096 ? row_choice<link ? 128 : 256, link ? 4 : 2, link ? 2 : 1, kIn32, kOut, kNorm>()
+             : n <= 8192 ? row_choice<link ? 256 : 512, link ? 4 : 2, link ? 2 : 1, kIn32, kOut, kNorm>() : row_choice<256, 8, 1, kIn32, kOut, kNorm>();
+    } else {
+        return n <= 512 ? row_choice<16, 4, 2, kIn32, kOut, kNorm>() : n <= 1024 ? row_choice<32, 4, 1, kIn32, kOut, kNorm>() : n <= 2048 ? row_choice<64, 4, 1, kIn32, kOut, kNorm>()
+             : n <= 4096 ? row_choice<128, 4, 1, kIn32, kOut, kNorm>() : n <= 8192 ? row_choice<link ? 128 : 256, link ? 8 : 4, link ? 2 : 1, kIn32, kOut, kNorm>()
+             : row_choice<link ? 256 : 512, link ? 8 : 4, link ? 2 : 1, kIn32, kOut, kNorm>();
+    }
 }
 // Layer norm of many rows of 257 to 16384 channels (8192 of fp32): CTAs that stay.  kernel null: too few rows to fill them several times, or rows of
 // another length.  (8-bit results take a third reduction a row, which more and smaller groups hide better: 8192 rows of 4096 35 us, here 38.)
@@ -238,19 +255,19 @@ static StreamChoice stream_choice(const Launch &L, long long rows, int sms) {
     return {xk::row_stream_kernel<G, V, kIn32, kOut>, Shape::cta, grid, Shape::slots * Shape::groups * bytes};
 }
 // ... of rows that are not whole chunks: bf16 only (16384 rows of 4095: 107 us one row a CTA, 72 here; of fp32 50 either way).
-template <int G, int kOut>
+template <int G, int A, int kOut>
 static StreamChoice stream_odd_choice(const Launch &L, long long rows, int sms) {
     const int grid = 512 / G * sms;
     if (rows < 4ll * grid) return {nullptr, 0, 0, 0};
-    return {xk::row_stream_odd_kernel<G, 4, false, kOut>, G, grid, 2 * (int)(align_up((size_t)L.C * 2, 16) + 16)};
+    return {xk::row_stream_odd_kernel<G, 4, A, false, kOut>, G, grid, 2 * (int)(align_up((size_t)L.C * 2, 16) + 16)};
 }
 template <int kOut>
 static StreamChoice stream_choice(const Launch &L, long long rows, int sms) {
     const int n = L.C;
     if (L.row_norm && n % 8 && n > 256 && n <= 16384 && !L.row_in_f32)
-        return n <= 1024 ? stream_odd_choice<32, kOut>(L, rows, sms) : n <= 2048 ? stream_odd_choice<64, kOut>(L, rows, sms)
-             : n <= 4096 ? stream_odd_choice<128, kOut>(L, rows, sms) : n <= 8192 ? stream_odd_choice<256, kOut>(L, rows, sms)
-             : stream_odd_choice<512, kOut>(L, rows, sms);
+        return n <= 1024 ? stream_odd_choice<32, 1, kOut>(L, rows, sms) : n <= 2048 ? stream_odd_choice<64, 2, kOut>(L, rows, sms)
+             : n <= 4096 ? stream_odd_choice<128, 1, kOut>(L, rows, sms) : n <= 8192 ? stream_odd_choice<256, 1, kOut>(L, rows, sms)
+             : stream_odd_choice<512, 1, kOut>(L, rows, sms);
     if (!L.row_norm || n % 8 || n <= 256 || n > (L.row_in_f32 ? 8192 : 16384)) return {nullptr, 0, 0, 0};
     if (L.row_in_f32)
         return n <= 512 ? stream_choice<32, 2, true, kOut>(L, rows, sms) : n <= 1024 ? stream_choice<64, 2, true, kOut>(L, rows, sms)

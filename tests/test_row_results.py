@@ -214,3 +214,56 @@ def test_more_than_2_to_30_rows_are_refused(h, w, batch):
     for build in (lambda g, x: norm(g, x, 1), lambda g, x: product(g, x, 1, 1), lambda g, x: g.add_logprob(x)[1]):
         assert refusal(lambda g: [(build(g, rows_in(g, F, 1, h, w)), F)], batch=batch) == xb.E_UNSUPPORTED
     compiled(lambda g: [(norm(g, rows_in(g, F, 1, 32768, 32768 // batch), 1), F)], batch=batch)
+
+
+# ---- one order of a row's sums -----------------------------------------------------------------------------------------------
+def normal_rows(rows, c, kind, key):
+    from row_util import rounded
+    rng = np.random.default_rng(key)
+    return rounded(rng.standard_normal((rows, c)) * np.exp(0.5 * rng.standard_normal(c)) + 0.5, kind)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,c,kind", [
+    (12000, 264, "bf16"), (9000, 512, "bf16"), (5003, 1032, "bf16"), (3700, 2048, "bf16"), (2400, 4096, "bf16"), (1300, 5000, "bf16"), (700, 12000, "bf16"), (300, 60, "bf16"),
+    (300, 192, "bf16"), (3000, 333, "bf16"), (9600, 333, "bf16"), (3000, 1111, "bf16"), (5000, 1111, "bf16"), (2401, 4095, "bf16"), (900, 5001, "bf16"), (1250, 5001, "bf16"),
+    (620, 9001, "bf16"), (300, 61, "bf16"), (40, 20001, "bf16"),
+    (12000, 264, "f32"), (5003, 1032, "f32"), (2400, 2048, "f32"), (1300, 4096, "f32"), (700, 8000, "f32"), (100, 9000, "f32"), (3000, 333, "f32"), (777, 1111, "f32"), (300, 4095, "f32"),
+    (300, 6001, "f32")])
+def test_link_of_norm_and_product_changes_no_bit(rows, c, kind):
+    """The sums of a row have one order, whichever kernel takes it: rows of the 8-bit values, scales and products are equal bit for bit."""
+    from row_util import Rows, to_device
+    rng = np.random.default_rng(c)
+    gamma, beta = (1 + 0.2 * rng.standard_normal(c)).astype(np.float32), (0.1 * rng.standard_normal(c)).astype(np.float32)
+    w, s = rng.integers(-127, 128, (24, c)).astype(np.int8), (0.002 + 0.001 * rng.random(24)).astype(np.float32)
+    x = to_device(normal_rows(rows, c, kind, rows), kind)
+
+    def build(g):
+        t = g.add_input(F if kind == "f32" else B, xb.LAYOUT_NHWC, c, 1, 1)
+        return [(g.add_qmatmul(g.add_op(xb.OP_LAYERNORM, [t], weight=gamma, bias=beta), w, s), 24, "f32")]
+    linked, plain = Rows(build, rows, link=True), Rows(build, rows)
+    assert [ch["kind"] for ch in linked.g.plan()["chains"]] == ["norm_qmatmul"]
+    assert [l["kind"] for l in plain.g.plan()["launches"]] == ["rows", "rows", "q8"]
+    (a,), (b,) = linked.run([x], rows), plain.run([x], rows)
+    assert np.array_equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,c,kind", [
+    (12000, 264, "bf16"), (9000, 512, "bf16"), (5003, 1032, "bf16"), (3700, 2048, "bf16"), (2400, 4096, "bf16"), (1300, 5000, "bf16"), (700, 12000, "bf16"), (9600, 333, "bf16"),
+    (5000, 1111, "bf16"), (2401, 4095, "bf16"), (1250, 5001, "bf16"), (620, 9001, "bf16"), (12000, 264, "f32"), (9000, 1000, "f32"), (2400, 2048, "f32"), (1300, 4096, "f32"), (700, 8000, "f32")])
+def test_norm_of_a_row_does_not_depend_on_the_number_of_rows(rows, c, kind):
+    """Enough rows for the CTAs that stay, and the first and last of them alone."""
+    from row_util import Rows, to_device
+    rng = np.random.default_rng(c)
+    gamma, beta = (1 + 0.2 * rng.standard_normal(c)).astype(np.float32), (0.1 * rng.standard_normal(c)).astype(np.float32)
+    x = normal_rows(rows, c, kind, rows)
+
+    def build(g):
+        t = g.add_input(F if kind == "f32" else B, xb.LAYOUT_NHWC, c, 1, 1)
+        return [(g.add_op(xb.OP_LAYERNORM, [t], weight=gamma, bias=beta), c, "f32")]
+    r = Rows(build, rows)
+    many, = r.run([to_device(x, kind)], rows)
+    for part in (slice(0, 100), slice(rows - 3, rows)):
+        few, = r.run([to_device(x[part], kind)], len(x[part]))
+        assert np.array_equal(few, many[part])
