@@ -324,7 +324,8 @@ XENOS_API xenos_status_t xenos_graph_selftest_wait_expiry(xenos_graph_t *g, void
 /* Write the compiled plan as JSON into `json` (capacity `cap`, always NUL-terminated when
  * cap > 0); *needed receives the length including the NUL.  Contents: fused operators,
  * chains with their Table 1 pattern, tiles, halos, grid, CTA -> tile rule, workspace
- * offsets, and modelled bytes / FLOPs per chain.  Deterministic: equal graphs and options
+ * offsets, and modelled bytes / FLOPs per chain.  Kernels and tiles are those of a pass over max_batch
+ * images; smaller batches may run other ones.  Deterministic: equal graphs and options
  * give byte-identical plans. */
 XENOS_API xenos_status_t xenos_graph_get_plan(const xenos_graph_t *g, char *json, size_t cap,
                                               size_t *needed);

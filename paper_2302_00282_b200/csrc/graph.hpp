@@ -280,6 +280,29 @@ inline int out_dim(int in, int k, int stride, int pad) {
 }
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
+// Layer norm of many rows of 257 to 16384 channels (8192 of fp32) by CTAs that stay: threads of a group (0: too few rows to fill them several times, or
+// rows of another length), groups of a CTA, CTAs, shared memory.  Rows that are not whole chunks of 8: bf16 only (16384 rows of 4095: 107 us one row a CTA, 72
+// here).  CTAs of an SM: as many as have some 64 KB of rows under way, 48 KB in small groups (measured, 268 MB in and out: 128 KB 52 us, 96 KB 47 to 50, 64 KB
+// 45.5, 32 KB 59), at most 640 threads.
+struct RowStream { int group = 0, groups = 1, grid = 0, smem = 0; };
+inline RowStream row_stream(int c, bool f32, long long rows, int sms) {
+    const bool odd = c % 8 != 0;
+    if (c <= 256 || c > (f32 ? (odd ? 0 : 8192) : 16384)) return RowStream();
+    RowStream s;
+    s.group = c <= 512 ? 32 : c <= 1024 ? (f32 ? 64 : 32) : c <= 2048 ? (f32 ? 128 : 64) : c <= 4096 ? (f32 ? 256 : 128) : c <= 8192 ? (f32 ? 512 : 256) : 512;
+    s.groups = s.group == 32 && !odd ? 4 : 1;
+    const int cta = s.group * s.groups, slots = 2 * s.groups;
+    if (odd) {
+        s.grid = 512 / cta * sms;
+        s.smem = slots * (int)(align_up((size_t)c * 2, 16) + 16);
+    } else {
+        const int row_bytes = c * (f32 ? 4 : 2), n = (s.group < 128 ? 48 : 64) * 1024 / (slots * row_bytes), most = cta >= 640 ? 1 : 640 / cta;
+        s.grid = (n < 1 ? 1 : n > most ? most : n) * sms;
+        s.smem = slots * row_bytes;
+    }
+    return rows < 4ll * s.grid * s.groups ? RowStream() : s;
+}
+
 // Rows, and values of all rows, up to which an 8-bit product goes through q8_small_kernel.
 constexpr int kQ8SmallRows = 16, kQ8SelfValues = 16384;
 inline bool q8_self(long long rows, int c) { return rows <= kQ8SmallRows && rows * ((c + 127) / 128 * 128) <= kQ8SelfValues; }

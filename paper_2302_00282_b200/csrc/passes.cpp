@@ -1975,8 +1975,13 @@ static void jarr(std::string &s, const char *k, const std::vector<int> &v, bool 
     s += "]"; if (comma) s += ",";
 }
 
-// The kernel a launch runs (a pool of windows up to 3 runs maxpool_kernel when its items fit 31 bits).
-static std::string kernel_of(const Launch &L) {
+// The kernel a launch runs for the largest batch (a pool of windows up to 3 runs maxpool_kernel when its items fit 31 bits).
+static std::string kernel_of(const Graph &g, const Launch &L) {
+    if (L.kind == LK_ROWS) {
+        const int n = L.row_out == 2 ? L.q_pitch : L.C;
+        const bool stay = L.row_norm && L.row_out != 2 && row_stream(L.C, L.row_in_f32, (long long)g.max_batch * L.rows_per_image, g.hw.sm_count).group;
+        return n > 16384 ? "row_long_kernel" : L.C % 8 ? (stay ? "row_stream_odd_kernel" : "row_odd_kernel") : stay ? "row_stream_kernel" : "row_kernel";
+    }
     if (L.kind == LK_GEMM)
         return L.fc_small ? "fc_small_kernel" : L.stem_tc ? "stem_tc_kernel" : L.conv_tc ? "conv_tc_kernel" : L.seg[0].mode == AM_DW ? "dw_tc_kernel" : "gemm_chain_kernel";
     if (L.kind == LK_GEMM2) return L.pair ? "pair_tc_kernel" : "chain2_kernel";
@@ -2030,7 +2035,7 @@ void emit_plan_json(Graph &g) {
         const Launch &L = g.launches[i];
         if (i) s += ",";
         s += "{";
-        jint(s, "id", (long long)i); jstr(s, "kind", lk[L.kind]); jstr(s, "kernel", kernel_of(L)); jint(s, "chain", L.chain); jarr(s, "nodes", L.nodes);
+        jint(s, "id", (long long)i); jstr(s, "kind", lk[L.kind]); jstr(s, "kernel", kernel_of(g, L)); jint(s, "chain", L.chain); jarr(s, "nodes", L.nodes);
         jint(s, "in0", L.in0); jint(s, "in1", L.in1); jint(s, "in2", L.in2); jint(s, "skip", L.skip); jint(s, "out", L.out);
         jint(s, "out_coff", L.out_coff); jint(s, "out_ctot", L.out_ctot);
         jint(s, "C", L.C); jint(s, "H", L.H); jint(s, "W", L.W); jint(s, "K", L.K); jint(s, "P", L.P); jint(s, "Q", L.Q);

@@ -353,12 +353,6 @@ template <int G, int V, bool kIn32> struct StreamShape {
     static constexpr int groups = G == 32 ? 4 : 1;
     static constexpr int slots = 2;
     static constexpr int resident = cta >= 512 ? 1 : 512 / cta;
-    // CTAs of an SM: as many as have some 64 KB of rows under way, 48 KB in small groups (measured, 268 MB in and out: 128 KB 52 us, 96 KB 47 to 50,
-    // 64 KB 45.5, 32 KB 59), at most 640 threads.
-    static int per_sm(int row_bytes) {
-        const int n = (G < 128 ? 48 : 64) * 1024 / (slots * groups * row_bytes), most = cta >= 640 ? 1 : 640 / cta;
-        return n < 1 ? 1 : n > most ? most : n;
-    }
 };
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");

@@ -244,42 +244,19 @@ static RowChoice row_choice(int n, bool vec) {
              : row_choice<link ? 256 : 512, link ? 8 : 4, link ? 2 : 1, kIn32, kOut, kNorm>();
     }
 }
-// Layer norm of many rows of 257 to 16384 channels (8192 of fp32): CTAs that stay.  kernel null: too few rows to fill them several times, or rows of
-// another length.  (8-bit results take a third reduction a row, which more and smaller groups hide better: 8192 rows of 4096 35 us, here 38.)
-struct StreamChoice { RowKernel kernel; int threads, grid, smem; };
-template <int G, int V, bool kIn32, int kOut>
-static StreamChoice stream_choice(const Launch &L, long long rows, int sms) {
-    typedef xk::StreamShape<G, V, kIn32> Shape;
-    const int bytes = L.C * (kIn32 ? 4 : 2), grid = Shape::per_sm(bytes) * sms;
-    if (rows < 4ll * grid * Shape::groups) return {nullptr, 0, 0, 0};
-    return {xk::row_stream_kernel<G, V, kIn32, kOut>, Shape::cta, grid, Shape::slots * Shape::groups * bytes};
-}
-// ... of rows that are not whole chunks: bf16 only (16384 rows of 4095: 107 us one row a CTA, 72 here; of fp32 50 either way).
-template <int G, int A, int kOut>
-static StreamChoice stream_odd_choice(const Launch &L, long long rows, int sms) {
-    const int grid = 512 / G * sms;
-    if (rows < 4ll * grid) return {nullptr, 0, 0, 0};
-    return {xk::row_stream_odd_kernel<G, 4, A, false, kOut>, G, grid, 2 * (int)(align_up((size_t)L.C * 2, 16) + 16)};
-}
+// The kernel of a layer norm's CTAs that stay (row_stream).  (8-bit results take a third reduction a row, which more and smaller groups hide better: 8192 rows of
+// 4096 35 us, here 38.)
 template <int kOut>
-static StreamChoice stream_choice(const Launch &L, long long rows, int sms) {
-    const int n = L.C;
-    if (L.row_norm && n % 8 && n > 256 && n <= 16384 && !L.row_in_f32)
-        return n <= 1024 ? stream_odd_choice<32, 1, kOut>(L, rows, sms) : n <= 2048 ? stream_odd_choice<64, 2, kOut>(L, rows, sms)
-             : n <= 4096 ? stream_odd_choice<128, 1, kOut>(L, rows, sms) : n <= 8192 ? stream_odd_choice<256, 1, kOut>(L, rows, sms)
-             : stream_odd_choice<512, 1, kOut>(L, rows, sms);
-    if (!L.row_norm || n % 8 || n <= 256 || n > (L.row_in_f32 ? 8192 : 16384)) return {nullptr, 0, 0, 0};
-    if (L.row_in_f32)
-        return n <= 512 ? stream_choice<32, 2, true, kOut>(L, rows, sms) : n <= 1024 ? stream_choice<64, 2, true, kOut>(L, rows, sms)
-             : n <= 2048 ? stream_choice<128, 2, true, kOut>(L, rows, sms) : n <= 4096 ? stream_choice<256, 2, true, kOut>(L, rows, sms)
-             : stream_choice<512, 2, true, kOut>(L, rows, sms);
-    return n <= 512 ? stream_choice<32, 2, false, kOut>(L, rows, sms) : n <= 1024 ? stream_choice<32, 4, false, kOut>(L, rows, sms)
-         : n <= 2048 ? stream_choice<64, 4, false, kOut>(L, rows, sms) : n <= 4096 ? stream_choice<128, 4, false, kOut>(L, rows, sms)
-         : n <= 8192 ? stream_choice<256, 4, false, kOut>(L, rows, sms) : stream_choice<512, 4, false, kOut>(L, rows, sms);
-}
-static StreamChoice stream_choice(const Launch &L, long long rows, int sms) {
-    if (L.row_out == xk::RO_Q8) return {nullptr, 0, 0, 0};
-    return L.row_out == xk::RO_F32 ? stream_choice<xk::RO_F32>(L, rows, sms) : stream_choice<xk::RO_BF16>(L, rows, sms);
+static RowKernel stream_kernel(int c, bool f32) {
+    if (c % 8)
+        return c <= 1024 ? xk::row_stream_odd_kernel<32, 4, 1, false, kOut> : c <= 2048 ? xk::row_stream_odd_kernel<64, 4, 2, false, kOut>
+             : c <= 4096 ? xk::row_stream_odd_kernel<128, 4, 1, false, kOut> : c <= 8192 ? xk::row_stream_odd_kernel<256, 4, 1, false, kOut>
+             : xk::row_stream_odd_kernel<512, 4, 1, false, kOut>;
+    if (f32)
+        return c <= 512 ? xk::row_stream_kernel<32, 2, true, kOut> : c <= 1024 ? xk::row_stream_kernel<64, 2, true, kOut> : c <= 2048 ? xk::row_stream_kernel<128, 2, true, kOut>
+             : c <= 4096 ? xk::row_stream_kernel<256, 2, true, kOut> : xk::row_stream_kernel<512, 2, true, kOut>;
+    return c <= 512 ? xk::row_stream_kernel<32, 2, false, kOut> : c <= 1024 ? xk::row_stream_kernel<32, 4, false, kOut> : c <= 2048 ? xk::row_stream_kernel<64, 4, false, kOut>
+         : c <= 4096 ? xk::row_stream_kernel<128, 4, false, kOut> : c <= 8192 ? xk::row_stream_kernel<256, 4, false, kOut> : xk::row_stream_kernel<512, 4, false, kOut>;
 }
 template <bool kIn32>
 static RowChoice row_choice(const Launch &L) {
@@ -750,9 +727,10 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
             p.scale = (float *)(scratch + L.q_scale_off);
             p.rows = (long long)N * L.rows_per_image; p.C = L.C; p.pitch = L.row_out == xk::RO_Q8 ? L.q_pitch : L.C; p.eps = L.eps;
             p.status = status; p.launch_id = (int)li;
-            const StreamChoice stay = stream_choice(L, p.rows, sms);
-            if (stay.kernel) {
-                le = to.pdl(stay.kernel, stay.grid, stay.threads, stay.smem, p);
+            const RowStream stay = L.row_norm && L.row_out != xk::RO_Q8 ? row_stream(L.C, L.row_in_f32, p.rows, sms) : RowStream();
+            if (stay.group) {
+                le = to.pdl(L.row_out == xk::RO_F32 ? stream_kernel<xk::RO_F32>(L.C, L.row_in_f32) : stream_kernel<xk::RO_BF16>(L.C, L.row_in_f32), stay.grid, stay.group * stay.groups,
+                            stay.smem, p);
                 break;
             }
             const RowChoice k = L.row_in_f32 ? row_choice<true>(L) : row_choice<false>(L);

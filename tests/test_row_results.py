@@ -267,3 +267,24 @@ def test_norm_of_a_row_does_not_depend_on_the_number_of_rows(rows, c, kind):
     for part in (slice(0, 100), slice(rows - 3, rows)):
         few, = r.run([to_device(x[part], kind)], len(x[part]))
         assert np.array_equal(few, many[part])
+
+
+# ---- plans -------------------------------------------------------------------------------------------------------------------
+def test_plan_names_the_kernels_of_rows():
+    """By length, type, number of rows and how rows leave."""
+    def names(rows, c, dtype=B, link=False, build=norm):
+        def f(g):
+            x = rows_in(g, dtype, c, 1, 1)
+            return [(product(g, norm(g, x, c), c, 8) if link else build(g, x, c), F)]
+        return [l["kernel"] for l in compiled(f, batch=rows, link=link).plan()["launches"]]
+    assert names(1, 1024) == ["row_kernel"] and names(100, 4096) == ["row_kernel"]
+    assert names(16384, 4096) == ["row_stream_kernel"] and names(16384, 1024, F) == ["row_stream_kernel"]
+    assert names(16384, 256) == ["row_kernel"] and names(40000, 8200, F) == ["row_kernel"]
+    assert names(50, 1111) == ["row_odd_kernel"] and names(16384, 1111, F) == ["row_odd_kernel"]
+    assert names(16384, 4095) == ["row_stream_odd_kernel"]
+    assert names(50, 16392) == ["row_long_kernel"] and names(50, 20001) == ["row_long_kernel"]
+    assert names(16384, 4096, link=True) == ["row_kernel", "q8_tc_kernel"]
+    assert names(16384, 4095, link=True) == ["row_odd_kernel", "q8_tc_kernel"]
+    assert names(40, 16300, build=lambda g, x, c: product(g, x, c, 8)) == ["row_odd_kernel", "q8_tc_kernel"]
+    assert names(40, 16385, build=lambda g, x, c: product(g, x, c, 8)) == ["row_long_kernel", "q8_tc_kernel"]
+    assert names(4, 64, build=lambda g, x, c: product(g, x, c, 8)) == ["q8_small_kernel"]
