@@ -159,7 +159,7 @@ xenos_status_t load_graph(Graph &g, const uint8_t *buf, size_t bytes, bool *comp
     for (const Tensor &t : g.tensors) {
         if (t.producer < -1 || t.producer >= O) return fail(g, XENOS_E_INVALID, "load: tensor producer out of range");
         for (int c : t.consumers) if (c < 0 || c >= O) return fail(g, XENOS_E_INVALID, "load: tensor consumer out of range");
-        if (t.c < 1 || t.h < 0 || t.w < 0) return fail(g, XENOS_E_INVALID, "load: tensor extent out of range");
+        if (t.c < 1 || t.h < 0 || t.w < 0 || (!t.is_vec && (t.h < 1 || t.w < 1))) return fail(g, XENOS_E_INVALID, "load: tensor extent out of range");
     }
     for (const Op &o : g.ops) {
         if (!tid(o.out)) return fail(g, XENOS_E_INVALID, "load: operator output out of range");

@@ -288,3 +288,64 @@ def test_plan_names_the_kernels_of_rows():
     assert names(40, 16300, build=lambda g, x, c: product(g, x, c, 8)) == ["row_odd_kernel", "q8_tc_kernel"]
     assert names(40, 16385, build=lambda g, x, c: product(g, x, c, 8)) == ["row_long_kernel", "q8_tc_kernel"]
     assert names(4, 64, build=lambda g, x, c: product(g, x, c, 8)) == ["q8_small_kernel"]
+
+
+# ---- stored graphs -----------------------------------------------------------------------------------------------------------
+def test_images_with_empty_maps_are_refused():
+    """An image with a right checksum whose input has no rows: the launch would divide by their number."""
+    g = xb.Graph()
+    x = g.add_input(F, xb.LAYOUT_NHWC, 9001, 77, 79)
+    g.mark_output(g.add_logprob(x)[1], F, xb.LAYOUT_NHWC)
+    img = bytearray(g.save()[:-8])
+    extent = (77).to_bytes(4, "little") + (79).to_bytes(4, "little")
+    places = [i for i in range(len(img) - 7) if img[i:i + 8] == extent]
+    assert len(places) == 2                                     # the scores' and the entropy's
+
+    def stored(h):
+        for i in places:
+            img[i:i + 4] = h.to_bytes(4, "little")
+        v = 1469598103934665603
+        for c in img:
+            v = (v ^ c) * 1099511628211 % (1 << 64)
+        return bytes(img) + v.to_bytes(8, "little")
+    xb.Graph.load(stored(78))
+    with pytest.raises(xb.XenosError) as e:
+        xb.Graph.load(stored(0))
+    assert e.value.code == xb.E_INVALID
+
+
+# ---- scores from the library's other heads -----------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("head", ["convolution", "depthwise", "fc", "long fc"])
+@pytest.mark.parametrize("batch", [1, 3, 40])
+def test_answers_read_fp32_scores_of_every_head(head, batch):
+    """Scores that leave the graph and scores that only LOGPROB reads are the same fp32 values: global averages behind a convolution or a depthwise chain, linked
+    or not, and fully connected layers, one with a reduction that is cut."""
+    from row_util import Rows, to_device
+    rng = np.random.default_rng(len(head) * 100 + batch)
+    w, wd = rng.standard_normal((104, 64, 1, 1)) * 0.2, rng.standard_normal((64, 1, 3, 3)) * 0.3
+    wf = rng.standard_normal((104, 2048 if head == "long fc" else 64)) * 0.1
+    wide = rng.standard_normal((2048, 64, 1, 1)) * 0.2
+
+    def build(scores):
+        def f(g):
+            x = rows_in(g, B, 64, 7, 7)
+            if head == "depthwise":
+                x = g.add_op(xb.OP_CONV, [x], cout=64, k=3, pad=1, groups=64, weight=wd, act=xb.ACT_RELU)
+            if head in ("convolution", "depthwise"):
+                z = g.add_op(xb.OP_POOL_GLOBAL_AVG, [g.add_op(xb.OP_CONV, [x], cout=104, k=1, weight=w, act=xb.ACT_RELU)])
+            else:
+                if head == "long fc":
+                    x = g.add_op(xb.OP_CONV, [x], cout=2048, k=1, weight=wide, act=xb.ACT_RELU)
+                z = g.add_op(xb.OP_FC, [g.add_op(xb.OP_POOL_GLOBAL_AVG, [x])], cout=104, k=1, weight=wf)
+            lp, ent, ids, tops = g.add_logprob(z, None, 4)
+            return [(ids, 4, "i32"), (tops, 4, "f32"), (ent, 1, "f32")] + ([(z, 104, "f32")] if scores else [])
+        return f
+    x = to_device(rng.standard_normal((batch, 7, 7, 64)), "bf16")
+    for link in (False, True):
+        *want, z = Rows(build(True), batch, link=link).run([x], batch)
+        assert np.isfinite(z).all() and z.std() > 0.01
+        order = np.argsort(-z, axis=1, kind="stable")[:, :4]
+        assert np.array_equal(want[0], order)
+        for u, v in zip(Rows(build(False), batch, link=link).run([x], batch), want):
+            assert np.array_equal(u, v)
