@@ -167,7 +167,9 @@ XENOS_API xenos_status_t xenos_graph_mark_output(xenos_graph_t *g, xenos_id_t te
  * in a batch (XENOS_E_UNSUPPORTED at compile).
  *
  * LAYERNORM goes through xenos_graph_add_op: weight = gamma [c], bias = beta [c] or NULL, bn_eps > 0, cout = c or 0 (XENOS_E_SHAPE if another).  The variance is the mean of the
- * squared deviations.  LAYERNORM -> QMATMUL is a link: the normalised row leaves as 8-bit values with its scale.
+ * squared deviations; a row whose squared deviations leave the range of fp32 (magnitudes from some 1e17 on) gives beta, or NaN where their sum does.  A row's result is
+ * the same bit for bit whatever the number of rows.  LAYERNORM -> QMATMUL is a link: the normalised row leaves as 8-bit values with its scale.  Its values are
+ * rounded to bf16 before they are rounded to 8 bits, also where the row came in as fp32: linked and not linked are equal bit for bit.
  *
  * QMATMUL: y[n] = act(sx * scale[n] * sum_k q[k] weight[n][k] + bias[n]) with q = round(127 x / a), halves to even, a = max_k |x[k]|,
  * sx = a / 127 for every row by itself; a row of zeros gives act(bias), a row with a NaN or an infinity gives NaN.  The sum of

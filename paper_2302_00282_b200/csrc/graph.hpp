@@ -281,8 +281,10 @@ inline int out_dim(int in, int k, int stride, int pad) {
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // Layer norm of many rows of 257 to 16384 channels (8192 of fp32) by CTAs that stay: threads of a group (0: too few rows to fill them several times, or
-// rows of another length), groups of a CTA, CTAs, shared memory.  Rows that are not whole chunks of 8: bf16 only (16384 rows of 4095: 107 us one row a CTA, 72
-// here).  CTAs of an SM: as many as have some 64 KB of rows under way, 48 KB in small groups (measured, 268 MB in and out: 128 KB 52 us, 96 KB 47 to 50, 64 KB
+// rows of another length), groups of a CTA, CTAs, shared memory.  Measured in turn with one row a group, us: bf16 16384 rows of 4096 44.9 here, 55.1 there; 8178 of
+// 8192 44.1 and 59.2; 65535 of 1000 49.7 and 53.0; 22333 of 3000 65.3 and 61.4.  fp32: 65535 of 264 24.7 and 31.9; 65535 of 1000 86 and 99; 11166 of 6000 112 and 124;
+// but 65535 of 512 61.6 and 49.3, 32714 of 2048 102 and 97, 16357 of 4096 114 and 102.  Rows that are not whole chunks of 8: bf16 only (16384 rows of 4095 107 us
+// one row a CTA, 69 here; in fp32 such CTAs take 96 against 87 there, 49 against 32 for 60000 of 333, 34 against 39 for 20000 of 1111).  CTAs of an SM: as many as have some 64 KB of rows under way, 48 KB in small groups (measured, 268 MB in and out: 128 KB 52 us, 96 KB 47 to 50, 64 KB
 // 45.5, 32 KB 59), at most 640 threads.
 struct RowStream { int group = 0, groups = 1, grid = 0, smem = 0; };
 inline RowStream row_stream(int c, bool f32, long long rows, int sms) {
@@ -309,7 +311,9 @@ inline bool q8_self(long long rows, int c) { return rows <= kQ8SmallRows && rows
 constexpr int kLpCtaEntries = 8192;      // entries above which a row of scores may have CTAs of 256 threads, and several of them
 
 // Channel tile of an 8-bit product in tiles of one CTA: modelled cycles.  A block of 128 deep takes the slower of the tensor pipe (2 cycles a
-// column) and the operands' way from L2 (75 bytes a cycle); a tile's fill and epilogue come on top.
+// column) and the operands' way from L2 (75 bytes a cycle); a tile's fill and epilogue come on top.  (Every width and pairs measured for 81 products of 40 to
+// 8192 rows, 512 to 8192 deep, of 1000 to 16384 channels: the choice is the fastest or within 1 % of it for 76; at worst 1024 x 1024 x 4096 12.5 us by 256
+// channels, 11.0 by 128, and 1024 x 4096 x 4096 22.7 by pairs, 21.0 by 256.)
 inline double q8_cycles(long long rows, int N, int kblocks, int units, int tile_n) {
     const double tiles = (double)((rows + 127) / 128) * ((N + tile_n - 1) / tile_n);
     const double block = tile_n * 2.0 > (16384 + tile_n * 128) / 75.0 ? tile_n * 2.0 : (16384 + tile_n * 128) / 75.0;
@@ -332,7 +336,7 @@ inline int q8_tile_n(const xenos_hw_info_t &hw, long long rows, int N, int kbloc
     return best;
 }
 // ... and of pairs of CTAs with tiles of 256 x 256, whose results leave slower than their few blocks are multiplied (1024 x 512 x 8192: 14.6 us by
-// pairs, 12.5 by CTAs with 256 channels; 2048 x 4096 x 4096: 34.2 and 35.1).
+// pairs, 12.4 by CTAs with 256 channels; 2048 x 4096 x 4096: 33.0 and 35.0; 8192 x 4096 x 8192: 195 and 223).
 inline double q8_pair_cycles(long long rows, int N, int kblocks, int units) {
     const double tiles = (double)((rows + 255) / 256) * ((N + 255) / 256);
     const int pairs = units / 2 < 1 ? 1 : units / 2;

@@ -15,8 +15,8 @@
 // maximum below the last one.
 // Entries are ordered by (value, index), which no two share: results do not depend on the order in which threads reach the list.
 //
-// A row is a warp's, 128 threads' or 256 threads' (what a row costs beside its entries, some 500 instructions a warp, is the less the fewer
-// warps share it; so the rule is the fewest that keep the SMs busy), and few long rows are cut over several CTAs (up to 16 a row): each leaves (m, S, T) and its
+// A row is a warp's, 128 threads' or 256 threads' (what a row costs beside its entries, 400 instructions a warp and as many again with the best entries, is the
+// less the fewer warps share it; so the rule is the fewest that keep the SMs busy), and few long rows are cut over several CTAs (up to 16 a row): each leaves (m, S, T) and its
 // k best in the workspace, the last to arrive joins them.
 #pragma once
 

@@ -10,15 +10,15 @@
 //   one CTA   tiles of 128 rows x 32..256 channels, for products whose larger tiles would leave SMs idle
 //   a pair    two CTAs of a cluster share a tile of 256 x 256 (cta_group::2): each brings its 128 rows of both operands, so a block of 128 deep
 //             takes 32 KB per SM for 512 cycles of the tensor pipe instead of 48 KB (L2 gives an SM some 75 bytes a cycle)
-// Results leave through 32-row boxes in shared memory by bulk tensor stores (16-byte pieces of rows stored by the threads: 4096 x 1024 x 16384 73.9 us
-// against 58 so); rows that are not whole 16-byte pieces leave element by element.
+// Results leave through 32-row boxes in shared memory by bulk tensor stores (4096 x 1024 x 16384: 69 us, 3 more where the threads store 16-byte pieces of
+// rows); rows that are not whole 16-byte pieces leave element by element (16383 channels: 123).
 //
 // q8_small_kernel (up to 16 rows): a pass over the weights, bound by their bytes.  A CTA owns 16 channels, its 8 warps share the
 // depth; mma.sync takes the channels as its 16 rows and the activation's rows as its 8 columns (tcgen05 has no shape that reads
 // weights from registers).  The weights (512 bytes of depth a warp and channel, and while those are used the next) are asked for before the predecessor is waited
 // for.  Each CTA stays for several sets of channels where there are many; it finds the rows' scales and
 // rounds the rows to shared memory by itself: no second launch, but work that every CTA repeats, so the rule is 16384 values in all (4096 x 4096: 4
-// rows 7.1 us here and 10.4 there; 16 rows 19 and 10.4).
+// rows 7.4 us here and 10.5 there; 16 rows 19 and 10.5).
 #pragma once
 
 #include "conv_tc.cuh"

@@ -244,8 +244,8 @@ static RowChoice row_choice(int n, bool vec) {
              : row_choice<link ? 256 : 512, link ? 8 : 4, link ? 2 : 1, kIn32, kOut, kNorm>();
     }
 }
-// The kernel of a layer norm's CTAs that stay (row_stream).  (8-bit results take a third reduction a row, which more and smaller groups hide better: 8192 rows of
-// 4096 35 us, here 38.)
+// The kernel of a layer norm's CTAs that stay (row_stream).  (Not for rows that leave as 8-bit values: their third reduction a row is hidden better by more groups.
+// Measured when those took 35 us for 8192 rows of 4096: 38 by CTAs that stay.)
 template <int kOut>
 static RowKernel stream_kernel(int c, bool f32) {
     if (c % 8)
@@ -795,7 +795,7 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
             const int max_chunks = L.C % per_chunk ? (L.C + 2 * per_chunk - 2) / per_chunk : L.C / per_chunk;
             p.parts = 1;
             if (L.lp_parts_max > 1) {
-                // few rows: CTAs enough for two a unit, each with a chunk for every thread at least
+                // few rows: CTAs enough for two a unit, each with four chunks for every thread at least, one step of them
                 const long long fill = 2ll * g.hw.sm_count / p.rows;
                 p.parts = (int)std::max(1ll, std::min(fill, std::min((long long)L.lp_parts_max, (long long)max_chunks / 1024)));
             }
@@ -803,7 +803,9 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
             p.part_mst = (float *)(ws + g.split_off);
             p.part_key = (unsigned long long *)(ws + g.split_off + (size_t)2 * g.hw.sm_count * 16);
             p.arrived = (unsigned *)(ws + L.split_cnt_off);
-            // fewer threads a row where the rows alone keep the SMs busy
+            // fewer threads a row where the rows alone keep the SMs busy.  us, five best: by a warp and by 128 threads, fp32: 4096 rows of 1000 8.2 and 15.3, of 2048
+            // 10.5 and 14.3, of 3000 13.5 and 17.9, but 1024 of 2048 6.4 and 6.3, of 3000 8.9 and 6.4, of 4096 11.2 and 6.2.  By 128 and by 256 (in parts), bf16:
+            // 300 of 8192 5.2 and 6.0; 444 of 32768 15.1 and 9.6, 700 16.5 and 13.5, 888 14.2 and 15.2, 1332 20.0 and 21.2; 888 of 131072 57 and 48
             if (L.C <= 2048) le = to.pdl(f32 ? xk::logprob_kernel<32, true> : xk::logprob_kernel<32, false>, (unsigned)((p.rows + 3) / 4), 128, 0, p);
             else if (L.C <= kLpCtaEntries || p.rows >= 6ll * g.hw.sm_count) le = to.pdl(f32 ? xk::logprob_kernel<128, true> : xk::logprob_kernel<128, false>, (unsigned)p.rows, 128, 0, p);
             else le = to.pdl(f32 ? xk::logprob_kernel<256, true> : xk::logprob_kernel<256, false>, (unsigned)(p.rows * p.parts), 256, 0, p);

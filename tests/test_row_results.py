@@ -349,3 +349,25 @@ def test_answers_read_fp32_scores_of_every_head(head, batch):
         assert np.array_equal(want[0], order)
         for u, v in zip(Rows(build(False), batch, link=link).run([x], batch), want):
             assert np.array_equal(u, v)
+
+
+# ---- the range of a layer norm -----------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("c", [64, 1111, 4096])
+def test_norm_of_rows_beyond_the_range_of_squares(c):
+    """Deviations whose squares are no fp32 numbers leave beta; rows whose sum is none leave NaN; the rows beside them are what they are alone."""
+    from row_util import Rows, to_device
+    rng = np.random.default_rng(c)
+    beta = rng.standard_normal(c).astype(np.float32)
+    x = rng.standard_normal((4, c))
+    x[1] *= 1e25
+    x[2] = 3e38
+
+    def build(g):
+        return [(g.add_op(xb.OP_LAYERNORM, [g.add_input(F, xb.LAYOUT_NHWC, c, 1, 1)], weight=np.ones(c), bias=beta), c, "f32")]
+    r = Rows(build, 4)
+    got, = r.run([to_device(x, "f32")], 4)
+    assert np.array_equal(got[1], beta.astype(np.float64)) and np.isnan(got[2]).all()
+    for i in (0, 3):
+        alone, = r.run([to_device(x[i:i + 1], "f32")], 1)
+        assert np.array_equal(alone[0], got[i]) and got[i].std() > 0.9
