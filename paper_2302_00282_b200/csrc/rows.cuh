@@ -500,8 +500,8 @@ row_odd_kernel(const RowParams p) {
 #pragma unroll
         for (int i = 0; i < 8 * V; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
         const RowScale sc = row_scale(row_max<G>(m, red[3]));
+        if (words && !live) return;
         if (live && t == 0) p.scale[row] = sc.scale;
-        uint32_t *to = reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(p.y) + row * p.pitch);      // (the pitch is a multiple of 128)
         // channels G apart: four threads with four channels each exchange halves, then bytes, and each has four channels that lie together
         const bool up2 = t & 2, up1 = t & 1;
 #pragma unroll
@@ -517,9 +517,10 @@ row_odd_kernel(const RowParams p) {
                 const uint32_t far1 = __shfl_xor_sync(0xffffffffu, w, 1);
                 w = up1 ? __byte_perm(far1, w, 0x7351) : __byte_perm(w, far1, 0x6240);
                 at = (i + (t & 3)) * G + (t & ~3);
+                if (!live) continue;
             }
-            // (rows are filled up to the pitch with zeros: x = 0 there)
-            if (live && at < p.pitch) to[at / 4] = w;
+            // (rows are filled up to the pitch, a multiple of 128, with zeros: x = 0 there)
+            if (at < p.pitch) *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(p.y) + row * p.pitch + at) = w;
         }
         return;
     }
