@@ -32,7 +32,7 @@ struct LogprobParams {
     const int *labels;
     float *lp, *entropy, *top_lp;          // null: not wanted
     int *top_id;
-    unsigned int *status;
+    unsigned int *bad_label;               // set where a label is outside its row
     long long rows;
     int V, L, k;
     int parts, part_chunks;                // CTAs per row; 16-byte chunks each of them takes
@@ -183,7 +183,7 @@ __device__ __forceinline__ void lp_finish(const LogprobParams &p, const LpRow<kI
         if (lab >= 0 && lab < p.V) r = ((l == t ? x0 : x.entry(lab)) - m) - ls;
         else if (lab != -1) {
             r = __uint_as_float(0x7fc00000u);
-            atomicCAS(p.status, 0u, kStatusBounds);
+            *p.bad_label = 1u;
         }
         p.lp[row * p.L + l] = r;
     }

@@ -786,7 +786,7 @@ static xenos_status_t issue_pass(Graph &g, int batch, const void *const *in, voi
             xk::LogprobParams p;
             p.x = ptr(L.in0); p.labels = (const int *)ptr(L.labels);
             p.lp = (float *)ptr(L.outx[0]); p.entropy = (float *)ptr(L.outx[1]); p.top_id = (int *)ptr(L.outx[2]); p.top_lp = (float *)ptr(L.outx[3]);
-            p.status = status;
+            p.bad_label = status + 1;
             p.rows = (long long)N * L.rows_per_image; p.V = L.C; p.L = L.n_labels; p.k = L.top;
             const bool f32 = L.row_in_f32;
             const int per_chunk = f32 ? 4 : 8;
@@ -1165,9 +1165,15 @@ xenos_status_t runtime_status(Graph &g, void *stream_v) {
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
     cudaError_t e = cudaStreamSynchronize(stream);
     if (e != cudaSuccess) return cuda_fail(g, "stream synchronize", e);
-    unsigned int word = 0;
+    unsigned int words[2] = {};           // what a kernel gave up or found wrong; whether a label was outside its row
     uint8_t *ws = static_cast<uint8_t *>(g.ws);
-    if ((e = cudaMemcpy(&word, ws + g.status_off, 4, cudaMemcpyDeviceToHost)) != cudaSuccess) return cuda_fail(g, "status read", e);
+    if ((e = cudaMemcpy(words, ws + g.status_off, sizeof words, cudaMemcpyDeviceToHost)) != cudaSuccess) return cuda_fail(g, "status read", e);
+    const unsigned int word = words[0];
+    if (word == 0 && words[1] != 0) {
+        // (a word of its own: such a run is whole, and its arrival counters may be at work in a pass that another stream has behind it)
+        cudaMemset(ws + g.status_off + 4, 0, 4);
+        return fail(g, XENOS_E_BOUNDS, "a label of a LOGPROB is outside its row of scores");
+    }
     if (word == 0) return XENOS_OK;
     cudaMemset(ws + g.status_off, 0, 256 + g.cnt_bytes);      // (the arrival counters of a run that gave up are stale too)
     int code = -(int)(word & 0xffu);

@@ -371,3 +371,44 @@ def test_norm_of_rows_beyond_the_range_of_squares(c):
     for i in (0, 3):
         alone, = r.run([to_device(x[i:i + 1], "f32")], 1)
         assert np.array_equal(alone[0], got[i]) and got[i].std() > 0.9
+
+
+# ---- status ------------------------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+def test_labels_outside_leave_the_arrival_counters_alone():
+    """A label outside its row is an error of the caller's: the status is cleared, the counters that a pass behind it may be using are not.  A run that gave
+    up clears both, and is reported before a label."""
+    import torch
+    from row_util import Rows, to_device
+    c, rows = 20000, 3
+    rng = np.random.default_rng(9)
+
+    def build(g):
+        t = g.add_input(F, xb.LAYOUT_NHWC, c, 1, 1)
+        lp, ent, ids, tops = g.add_logprob(t, g.add_input(xb.DTYPE_I32, xb.LAYOUT_NHWC, 1, 1, 1), 4)
+        return [(lp, 1, "f32"), (ids, 4, "i32"), (tops, 4, "f32")]
+    r = Rows(build, rows)
+    words = r.ws.view(torch.int32)              # no parameters: the status words come first, the counters behind 256 bytes
+    assert not words[:64].any() and not words[64:64 + 2 * 148].any()
+    x = to_device(rng.standard_normal((rows, c)), "f32")
+    good, bad = (to_device(np.array(v, np.int32)[:, None], "i32") for v in ([5, -1, 19999], [5, 20000, -2]))
+    want = r.run([x, good], rows)
+    last = 64 + 2 * 148 - 1                     # the counter of a row that these runs do not have
+    words[last] = 7
+
+    def status():
+        try:
+            r.g.status(r.stream)
+            return xb.XENOS_OK
+        except xb.XenosError as e:
+            return e.code
+    got = r.run([x, bad], rows, status=False)
+    assert status() == xb.E_BOUNDS and int(words[last]) == 7 and status() == xb.XENOS_OK
+    assert got[0][0, 0] == want[0][0, 0] and np.isnan(got[0][1:]).all()
+    for u, v in zip(r.run([x, good], rows), want):
+        assert np.array_equal(u, v)
+    r.run([x, bad], rows, status=False)
+    r.g.selftest_wait_expiry(r.stream)
+    assert status() == xb.E_TIMEOUT and int(words[last]) == 0 and status() == xb.XENOS_OK
+    for u, v in zip(r.run([x, good], rows), want):
+        assert np.array_equal(u, v)
