@@ -54,8 +54,7 @@ struct Node {
     std::vector<float> b;         // folded bias [cout] (zeros when the op had none)
     std::vector<int> user_ops;    // indices of the user ops folded into this node
     int chain = -1;
-    std::vector<int8_t> q;        // qmatmul: weights [cout][cin], scales in w; layer norm: w = gamma, b = beta
-    float eps = 0;
+    float eps = 0;                // layer norm: w = gamma, b = beta (qmatmul: w = scales, the weights stay with the user's operator)
     int top = 0, outs[4] = {-1, -1, -1, -1};      // logprob
     bool from_matmul = false;     // an x.matmul with a constant right operand (lowered like a pointwise conv / fc)
 };

@@ -99,7 +99,6 @@ xenos_status_t prefuse(Graph &g) {
             n.in = op.in; n.out = op.out;
             n.cin = x.c; n.cout = g.tensors[op.out].c; n.act = op.act; n.eps = op.eps;
             n.w = op.kind == XENOS_OP_LAYERNORM ? op.w : op.gamma;
-            n.q = op.q;
             n.b.assign(n.cout, 0.0f);
             if (op.has_bias) n.b = op.bias;
             n.user_ops.push_back(oi);
@@ -551,7 +550,7 @@ struct Lower {
     }
     double node_param_bytes(const Node &n) const {
         if (n.w.empty()) return 0;
-        if (n.kind == NK_NORM || n.kind == NK_QMATMUL) return (double)n.q.size() + 4.0 * (n.w.size() + n.b.size());
+        if (n.kind == NK_NORM || n.kind == NK_QMATMUL) return (n.kind == NK_QMATMUL ? (double)n.cout * n.cin : 0.0) + 4.0 * (n.w.size() + n.b.size());
         return (double)n.w.size() * esize() + 4.0 * n.b.size();
     }
 
@@ -1637,7 +1636,8 @@ struct Lower {
         L.kblocks = L.q_pitch / 128;
         // weights [cout][pitch], zeros behind a row: the depth is whole blocks
         L.w_off = blob_reserve(g, (size_t)n.cout * L.q_pitch);
-        for (int o = 0; o < n.cout; ++o) std::memcpy(g.param_blob.data() + L.w_off + (size_t)o * L.q_pitch, n.q.data() + (size_t)o * n.cin, n.cin);
+        const std::vector<int8_t> &q = g.ops[n.user_ops[0]].q;
+        for (int o = 0; o < n.cout; ++o) std::memcpy(g.param_blob.data() + L.w_off + (size_t)o * L.q_pitch, q.data() + (size_t)o * n.cin, n.cin);
         L.w2_off = put_f32(n.w); L.b_off = put_f32(n.b);
         L.flops = 2.0 * node_macs(n);
         L.bytes = tbytes(n.out) + node_param_bytes(n);

@@ -412,3 +412,30 @@ def test_labels_outside_leave_the_arrival_counters_alone():
     assert status() == xb.E_TIMEOUT and int(words[last]) == 0 and status() == xb.XENOS_OK
     for u, v in zip(r.run([x, good], rows), want):
         assert np.array_equal(u, v)
+
+
+# ---- host memory -------------------------------------------------------------------------------------------------------------
+def test_compiled_8_bit_weights_are_held_twice():
+    """What was given, for a stored graph, and what a binding uploads; no third time."""
+    import os
+    import subprocess
+    import sys
+    program = """
+import numpy as np, resource
+from paper_2302_00282_b200 import binding as xb
+def graph(n, c):
+    g = xb.Graph()
+    x = g.add_input(xb.DTYPE_BF16, xb.LAYOUT_NHWC, c, 1, 1)
+    g.mark_output(g.add_qmatmul(x, w[:n, :c], np.ones(n)), xb.DTYPE_F32, xb.LAYOUT_NHWC)
+    g.compile(4, xb.PRECISION_BF16_TENSOR)
+    return g
+def now():
+    return int(open('/proc/self/statm').read().split()[1]) * resource.getpagesize()
+w = np.ones((16384, 8192), np.int8)
+graph(8, 64)
+before = now()
+g = graph(16384, 8192)
+print((now() - before) / w.nbytes)
+"""
+    out = subprocess.run([sys.executable, "-c", program], check=True, capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert 1.5 < float(out.stdout) < 2.5
