@@ -160,6 +160,8 @@ struct LinkCtx {
         return cons[t][0];
     }
     int rows(int n) const { const Tensor &t = g.tensors[g.nodes[n].out]; return t.h * t.w; }
+    // whether node n reads an NCHW image (of any number of channels), which only a convolution that starts a chain does
+    bool image(int n) const { const Tensor &t = g.tensors[g.nodes[n].in[0]]; return t.input_slot >= 0 && t.io_layout == XENOS_LAYOUT_NCHW; }
 };
 
 // Max pools that stem_tc_kernel forms row by row, over a map of `rows` rows: windows overlap by one row at most, and no two end with
@@ -290,7 +292,7 @@ static bool try_match(const LinkCtx &cx, int a, Allowed allowed, Chain &out, boo
         const Node &E0 = g.nodes[e0], &E1 = g.nodes[e1];
         if (E0.kind != NK_CONV || E1.kind != NK_CONV || E0.in[0] != E1.in[0]) return false;
         if (cx.sole(e0) != a || cx.sole(e1) != a) return false;
-        if (E0.act != E1.act || E0.stride != 1 || E1.stride != 1 || E0.cin % 8) return false;
+        if (E0.act != E1.act || E0.stride != 1 || E1.stride != 1 || E0.cin % 8 || cx.image(e0)) return false;
         auto shape_ok = [](const Node &n) { return (n.k == 1 && n.pad == 0) || (n.k == 3 && n.pad == 1); };
         if (!shape_ok(E0) || !shape_ok(E1) || (E0.k == 1 && E1.k == 1)) return false;
         if (E0.cout % 8 || E1.cout % 8) return false;
@@ -380,7 +382,7 @@ static bool try_match(const LinkCtx &cx, int a, Allowed allowed, Chain &out, boo
             // the shortcut's own 1x1 convolution joins the chain as a second K segment
             if (p >= 0 && p != a && allowed(p) && g.nodes[p].kind == NK_CONV && g.nodes[p].k == 1 &&
                 g.nodes[p].pad == 0 && g.nodes[p].act == XENOS_ACT_NONE && A.act == XENOS_ACT_NONE &&
-                cx.sole(p) == b && g.nodes[p].cin % 8 == 0 && g.nodes[p].chain < 0) {
+                cx.sole(p) == b && g.nodes[p].cin % 8 == 0 && !cx.image(p) && g.nodes[p].chain < 0) {
                 out.nodes.push_back(p);
                 out.pattern = "shortcut connection (ConvX -> {... -> ConvY ; ConvZ})";
             }

@@ -439,3 +439,56 @@ print((now() - before) / w.nbytes)
 """
     out = subprocess.run([sys.executable, "-c", program], check=True, capture_output=True, text=True, cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     assert 1.5 < float(out.stdout) < 2.5
+
+
+# ---- images beside other inputs ----------------------------------------------------------------------------------------------
+def conv_of(g, x, c, n=64, k=1):
+    return g.add_op(xb.OP_CONV, [x], cout=n, k=k, pad=k // 2, weight=np.random.default_rng(c * 10 + k).standard_normal((n, c, k, k)) * 0.2)
+
+
+def shortcut_of_image(dtype, c):
+    def f(g):
+        x, image = rows_in(g, B, 64, 4, 4), g.add_input(dtype, xb.LAYOUT_NCHW, c, 4, 4)
+        return [(g.add_op(xb.OP_ADD, [conv_of(g, x, 64), conv_of(g, image, c)]), B)]
+    return f
+
+
+def expand_of_image(dtype, c):
+    def f(g):
+        image = g.add_input(dtype, xb.LAYOUT_NCHW, c, 4, 4)
+        return [(g.add_op(xb.OP_CONCAT, [conv_of(g, image, c), conv_of(g, image, c, k=3)]), B)]
+    return f
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("c", [3, 8, 64])
+def test_links_leave_convolutions_of_images_alone(dtype, c):
+    """A convolution that reads an NCHW image joins no chain as its shortcut or as one of two expansions: those kernels read NHWC."""
+    for build in (shortcut_of_image, expand_of_image):
+        linked, plain = compiled(build(dtype, c), link=True).plan(), compiled(build(dtype, c)).plan()
+
+        def starts(p):
+            return sorted(l["kernel"] for l in p["launches"] if l["kernel"] in ("gemm_chain_kernel", "stem3x3_kernel", "stem_tc_kernel"))
+        assert starts(linked) == starts(plain) and starts(plain)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("c", [3, 8, 64])
+def test_linked_shortcut_of_an_image(dtype, c):
+    import torch
+    from row_util import Rows, rounded, to_device
+    rng = np.random.default_rng(c)
+    kind = "f32" if dtype == F else "bf16"
+    x, image = rounded(rng.standard_normal((3, 4, 4, 64)), "bf16"), rounded(rng.standard_normal((3, c, 4, 4)), kind)
+    w = [rounded(np.random.default_rng(n * 10 + 1).standard_normal((64, n, 1, 1)) * 0.2, "bf16").reshape(64, n) for n in (64, c)]
+    # (an fp32 image is rounded to bf16 in front of the product; half a step each, and one of the stored shortcut, of the result)
+    a, b = x @ w[0].T, rounded(image, "bf16").transpose(0, 2, 3, 1) @ w[1].T
+    tol = 2.0 ** -8 * (np.abs(a + b) + np.abs(b)) + 1e-4 * (np.abs(x) @ np.abs(w[0]).T)
+    for link in (False, True):
+        def build(g):
+            return [(shortcut_of_image(dtype, c)(g)[0][0], 64, "bf16")]
+        got, = Rows(build, 3, pixels=(4, 4), link=link).run([to_device(x, "bf16"), to_device(image, kind)], 3)
+        slack = 0 if link else 2.0 ** -8 * np.abs(a)            # (unlinked: the other operand is stored, too)
+        assert (np.abs(got.reshape(3, 4, 4, 64) - (a + b)) <= tol + slack).all()
+    torch.cuda.synchronize()
