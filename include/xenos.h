@@ -139,8 +139,8 @@ XENOS_API xenos_status_t xenos_graph_create(const xenos_hw_info_t *hw, xenos_gra
  * FP32_CUDA_CORE graphs take F32 NCHW; BF16_TENSOR graphs take F32 or BF16 NCHW when the
  * input feeds a convolution with fewer than 8 input channels (an image), BF16 NHWC with a
  * channel count that is a multiple of 8 otherwise.  Inputs that only row operators read may be
- * F32 or BF16 NHWC with any channel count (NCHW when h = w = 1, which is the same memory); compile refuses one that
- * another operator reads as well (XENOS_E_UNSUPPORTED).  The labels of a LOGPROB are I32 NHWC in either precision. */
+ * F32 or BF16 NHWC with any channel count (NCHW when h = w = 1, which is the same memory).  Compile refuses an F32 input
+ * that another operator reads as well, and an NCHW input that an operator other than a dense convolution reads (XENOS_E_UNSUPPORTED).  The labels of a LOGPROB are I32 NHWC in either precision. */
 XENOS_API xenos_status_t xenos_graph_add_input(xenos_graph_t *g, int32_t dtype, int32_t layout,
                                                int32_t c, int32_t h, int32_t w, xenos_id_t *tensor);
 

@@ -1854,6 +1854,8 @@ static xenos_status_t check_operands(Graph &g) {
             if (elem_dtype(g, t) != XENOS_DTYPE_BF16)
                 return fail(g, XENOS_E_UNSUPPORTED, "an F32 input, or an F32 output of the graph, is read by an operator that takes bf16 (row operators take either)");
             if (!x.is_vec && x.c % 8) return fail(g, XENOS_E_UNSUPPORTED, "bf16 NHWC tensors need a channel count that is a multiple of 8");
+            if (x.input_slot >= 0 && x.io_layout == XENOS_LAYOUT_NCHW && x.rows() > 1)
+                return fail(g, XENOS_E_UNSUPPORTED, "an NCHW input of more than one pixel is read by an operator that is no dense convolution");
         }
     }
     return XENOS_OK;

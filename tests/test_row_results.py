@@ -492,3 +492,26 @@ def test_linked_shortcut_of_an_image(dtype, c):
         slack = 0 if link else 2.0 ** -8 * np.abs(a)            # (unlinked: the other operand is stored, too)
         assert (np.abs(got.reshape(3, 4, 4, 64) - (a + b)) <= tol + slack).all()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("link", [False, True])
+@pytest.mark.parametrize("reader", [r for r in F32_READERS if r not in ("convolution", "shortcut convolution")])
+def test_nchw_inputs_are_for_dense_convolutions_alone(reader, link):
+    """Their kernels would take the planes of an image for pixels; one pixel is the same memory either way."""
+    def build(layout, side):
+        def f(g):
+            x = g.add_input(B, layout, 64, side, side)
+            y = rows_in(g, B, 64, side, side)
+            code = {"add": xb.OP_ADD, "add, other order": xb.OP_ADD, "mul": xb.OP_MUL, "concat": xb.OP_CONCAT}.get(reader)
+            if code is not None:
+                return [(g.add_op(code, [y, x] if reader != "add, other order" else [x, y]), B)]
+            if reader == "mac":
+                return [(g.add_op(xb.OP_MAC, [y, y, x]), B)]
+            if reader == "shortcut":
+                return [(g.add_op(xb.OP_ADD, [conv(g, y), x]), B)]
+            return [F32_READERS[reader](g, x)]
+        return f
+    assert refusal(build(xb.LAYOUT_NCHW, 4), link=link) == xb.E_UNSUPPORTED
+    compiled(build(xb.LAYOUT_NHWC, 4), link=link)
+    if "pool" not in reader and reader != "depthwise":
+        compiled(build(xb.LAYOUT_NCHW, 1), link=link)
